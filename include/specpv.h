@@ -311,6 +311,89 @@ int specpv_commit_accepted_layers(const specpv_kv *const *kv, void *const *buf_k
                                   const specpv_lists *lists, int32_t *dropped,
                                   void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- the cache in 4 bits ----------------------------------------------------------------
+ *
+ * A packed cache holds rows of K and V as E2M1 values (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign; the low nibble of byte i is
+ * channel 2 i) under one power of two 2^e for every 32 channels, stored as the byte e + 127: 4.25 bits a channel.  2^e is the
+ * smallest power of two under which the group's largest magnitude is at most 7, with -124 <= e <= 125; a value is |x| / 2^e rounded to
+ * nearest, ties to the even code, at most 6, with x's sign.  A group with an infinity or NaN in it has the byte 255 and stands
+ * for NaNs.  Values are exact in bf16, so what reads the cache computes with exactly the values that it stands for.
+ * N(0, 1) rows keep 11 % of their rms as error.
+ *
+ * k, v: codes; element row (b, t, g) of D / 2 bytes lies at base + b*stride_b + g*stride_h + t*stride_t (strides in BYTES, multiples of 16 and
+ * of D / 2; the codes' base 16-byte aligned).  k_scale, v_scale: its D / 32 bytes lie at base + (b*stride_b + g*stride_h + t*stride_t) / 16 (the base
+ * 4-byte aligned).  dtype: of the queries, draft rows, summaries and outputs that go with the cache.  Rows t >= ctx_len[b] are never read. */
+typedef struct specpv_packed_kv {
+    void *k, *v, *k_scale, *v_scale;
+    int64_t stride_b, stride_h, stride_t;
+    const int32_t *ctx_len; /* device, [batch]: L_b                                      */
+    int32_t batch, n_kv_heads, head_dim, block_size;
+    int32_t max_blocks;
+    specpv_dtype dtype;
+} specpv_packed_kv;
+
+/* Rows of src (an ordinary cache, a chunk of a prompt, the draft's buffer) into a packed cache.  For sequence b and
+ * i = 0 .. n_b - 1 token dst_begin[b] + i of dst becomes source row
+ *   src_rows[b, i]        ([batch, max_rows]; accepted candidates, for instance), or, src_rows == NULL,
+ *   src_begin[b] + i;
+ * n_b = n_rows[b], or where n_rows == NULL max_rows with src_rows and src->ctx_len[b] - src_begin[b] without; at most max_rows.
+ * dst_begin, src_begin, n_rows (device, [batch]) may be NULL (0, 0, as above); src_rows excludes src_begin.  Source rows outside
+ * 0 .. src->ctx_len[b] - 1 and tokens outside of dst (max_blocks * block_size) are left out, their places left as they were.
+ * dst->ctx_len is neither read nor written: the caller moves it on, as it does n_pending and the like.
+ * kmax, kmin (both or neither; [batch, Hkv, dst max_blocks, D] in the shared dtype): the summaries (eq. 1) of the blocks of dst that
+ * receive a token, of the source's keys, unrounded: of the new rows alone in a block that dst_begin[b] does not lie behind the
+ * start of, else of those and what the entries held.
+ * src and dst share batch, Hkv, D and dtype; block sizes and strides are each one's own. */
+int specpv_pack_tokens(const specpv_kv *src, const int32_t *src_begin, const int32_t *src_rows, const int32_t *n_rows, int32_t max_rows,
+                       const specpv_packed_kv *dst, const int32_t *dst_begin, void *kmax, void *kmin, void *stream);
+
+/* specpv_workspace_bytes, specpv_select_blocks and specpv_partial_verify_attn for a packed cache; arguments and results are
+ * theirs (all tree nodes that are keys only lie in kd / vd, in the shared dtype).  One workspace, zero-filled once, serves
+ * packed and ordinary calls if it has the larger size.  fp32 queries and weights are taken in full (24 bits); bf16 weights are
+ * rounded to bf16 in front of the product with V, as by the ordinary calls, and at head dim 128 the pieces' results travel as fp16 like theirs:
+ * V entries beyond +-65504 are clamped, and results below 2^-14 are exact to 2^-25. */
+size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tree *tree, const specpv_select_cfg *cfg);
+int specpv_packed_select_blocks(const specpv_packed_kv *kv, const specpv_tree *tree, const void *kmax, const void *kmin,
+                                const specpv_select_cfg *cfg, int32_t *sel_idx, int32_t *sel_count, float *scores,
+                                void *workspace, size_t workspace_bytes, void *stream);
+int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tree,
+                              const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel, void *out, float *lse,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* specpv_gather_blocks out of a packed cache: rows in its dtype.  sel_idx == NULL: every block in order, out_k / out_v
+ * [batch, Hkv, max_blocks * B, D] (n_sel is ignored), zeros from L_b on. */
+int specpv_packed_gather_blocks(const specpv_packed_kv *kv, const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel,
+                                void *out_k, void *out_v, int32_t *out_len, void *stream);
+
+/* ---- eviction by accumulated attention weight ---------------------------------------------
+ *
+ * What a pass's query rows attended: for every cached token t < L_b of KV head g
+ *   weights[b, g, t] += sum over the rows r of exp(q_r . k_t / sqrt(D) - lse_r),
+ * over the G query heads of the nodes that count: nodes [batch, max_nodes] holds n_nodes[b] query rows of the tree each (the
+ * accepted path as specpv_commit_accepted takes it: 0 is the first query node, n_key_only; entries outside 0 .. Mq - 1 are ignored, one
+ * that is listed twice counts twice), or, nodes == NULL, of all Mq.  With sel_idx only the tokens of the listed blocks (one listed m
+ * times is added to m times, as the attention attends it m times).  lse [batch, Mq, Hq] is what the attention over these keys gave;
+ * a row with -inf adds nothing.  Of the tree only q, M, n_q_heads and n_key_only are read; the draft's own keys have no weights.
+ * weights [batch, Hkv, max_blocks * B] fp32, the caller's, zero for tokens that nothing has looked at; entries t >= L_b are left as they
+ * are.  The same inputs give the same bits. */
+int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, const float *lse,
+                              const int32_t *nodes, const int32_t *n_nodes, int32_t max_nodes,
+                              const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel, float *weights, void *stream);
+
+/* Tokens that stay, and a cache of only those.  Of every (sequence, KV head): the first n_sink, the last n_recent and of the rest the k_tokens of
+ * largest weight (of equal ones the earlier; NaN below everything); all of them where L_b <= n = n_sink + k_tokens + n_recent.
+ *   keep_idx [batch, Hkv, n]: the kept tokens, ascending, -1 behind them;
+ *   rows 0 .. of dst->k, dst->v become theirs, in that order; dst->ctx_len[b] (written) = min(L_b, n); rows behind are left as they were;
+ *   dst_weights (may be NULL) [batch, Hkv, dst max_blocks * B]: their weights, zeros behind.
+ * Keys keep the positions they were rotated for: attention over dst is attention over the kept tokens.  dst shares batch, Hkv, D and
+ * dtype with kv, has room for n tokens, and none of its memory (ctx_len included) is kv's: one spare cache serves all layers in turn.
+ * Summaries and kept-block lists of dst are the caller's to rebuild.
+ * Workspace: specpv_evict_workspace_bytes(kv), zero-filled once (specpv_workspace_bytes), shared with other calls like any. */
+size_t specpv_evict_workspace_bytes(const specpv_kv *kv);
+int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sink, int32_t n_recent, int32_t k_tokens,
+                        const specpv_kv *dst, float *dst_weights, int32_t *keep_idx,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
 /* Testing and measuring aid, process-wide (not per thread, not per stream): how
  * specpv_partial_verify_attn runs the shapes that its eight-wavefront kernel takes (bf16, head dim
  * 128, short token ranges).

@@ -26,7 +26,9 @@ MODE_FULL, MODE_PARTIAL, MODE_REFRESH = 0, 1, 2
 
 EXPORTS = ["specpv_workspace_bytes", "specpv_block_summarize", "specpv_select_blocks",
            "specpv_partial_verify_attn", "specpv_partial_verify_attn_static", "specpv_full_verify_refresh", "specpv_gather_blocks", "specpv_select_mode",
-           "specpv_extend_parents", "specpv_commit_accepted", "specpv_commit_accepted_layers", "specpv_strerror",
+           "specpv_extend_parents", "specpv_commit_accepted", "specpv_commit_accepted_layers", "specpv_pack_tokens", "specpv_packed_workspace_bytes",
+           "specpv_packed_select_blocks", "specpv_packed_verify_attn", "specpv_packed_gather_blocks", "specpv_accumulate_weights",
+           "specpv_evict_workspace_bytes", "specpv_evict_tokens", "specpv_strerror",
            "specpv_last_hip_error", "specpv_version", "specpv_debug_set_route", "specpv_debug_set_select_route",
            "specpv_debug_set_timeline"]
 
@@ -39,6 +41,14 @@ class SpecPVError(RuntimeError):
 
 class _KV(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+                ("ctx_len", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block_size", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("dtype", ctypes.c_int)]
+
+
+class _PackedKV(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
                 ("ctx_len", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
@@ -69,7 +79,9 @@ _lib = None
 _native = None
 # the library's functions in the order of the extension's table
 _TABLE = ["specpv_block_summarize", "specpv_select_blocks", "specpv_partial_verify_attn", "specpv_partial_verify_attn_static",
-          "specpv_full_verify_refresh", "specpv_gather_blocks", "specpv_commit_accepted", "specpv_commit_accepted_layers"]
+          "specpv_full_verify_refresh", "specpv_gather_blocks", "specpv_commit_accepted", "specpv_commit_accepted_layers",
+          "specpv_pack_tokens", "specpv_packed_select_blocks", "specpv_packed_verify_attn", "specpv_packed_gather_blocks",
+          "specpv_accumulate_weights", "specpv_evict_tokens"]
 
 
 def lib_path():
@@ -118,6 +130,22 @@ def load():
     lib.specpv_commit_accepted_layers.restype = ctypes.c_int
     lib.specpv_commit_accepted_layers.argtypes = [P(P(_KV)), P(vp), P(vp), i32, i32, i32, vp, vp, vp, i32, ctypes.c_int,
                                                   P(vp), P(vp), P(_Lists), vp, vp, sz, vp]
+    lib.specpv_pack_tokens.restype = ctypes.c_int
+    lib.specpv_pack_tokens.argtypes = [P(_KV), vp, vp, vp, i32, P(_PackedKV), vp, vp, vp, vp]
+    lib.specpv_packed_workspace_bytes.restype = sz
+    lib.specpv_packed_workspace_bytes.argtypes = [P(_PackedKV), P(_Tree), P(_Cfg)]
+    lib.specpv_packed_select_blocks.restype = ctypes.c_int
+    lib.specpv_packed_select_blocks.argtypes = [P(_PackedKV), P(_Tree), vp, vp, P(_Cfg), vp, vp, vp, vp, sz, vp]
+    lib.specpv_packed_verify_attn.restype = ctypes.c_int
+    lib.specpv_packed_verify_attn.argtypes = [P(_PackedKV), P(_Tree), vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.specpv_packed_gather_blocks.restype = ctypes.c_int
+    lib.specpv_packed_gather_blocks.argtypes = [P(_PackedKV), vp, vp, i32, vp, vp, vp, vp]
+    lib.specpv_accumulate_weights.restype = ctypes.c_int
+    lib.specpv_accumulate_weights.argtypes = [P(_KV), P(_Tree), vp, vp, vp, i32, vp, vp, i32, vp, vp]
+    lib.specpv_evict_workspace_bytes.restype = sz
+    lib.specpv_evict_workspace_bytes.argtypes = [P(_KV)]
+    lib.specpv_evict_tokens.restype = ctypes.c_int
+    lib.specpv_evict_tokens.argtypes = [P(_KV), vp, i32, i32, i32, P(_KV), vp, vp, vp, sz, vp]
     lib.specpv_debug_set_route.restype = ctypes.c_int
     lib.specpv_debug_set_route.argtypes = [ctypes.c_int]
     lib.specpv_debug_set_select_route.restype = ctypes.c_int
@@ -191,6 +219,47 @@ class KV:
         self.dtype = k.dtype
         self.c = _KV(k.data_ptr(), v.data_ptr(), sb, sh, st, _ptr(ctx_len, torch.int32, "ctx_len").value,
                      batch, hkv, D, self.B, self.max_blocks, _DTYPE[k.dtype])
+
+    def summary_shape(self):
+        return (self.batch, self.Hkv, self.max_blocks, self.D)
+
+
+class PackedKV:
+    """One layer's KV cache in 4 bits (descriptor `specpv_packed_kv`).
+    k, v: uint8 codes [batch, Hkv, T, D / 2] (layout="bhtd") or [batch, T, Hkv, D / 2] ("bthd"); k_scale, v_scale: uint8
+    [.., D / 32] beside them, their strides a sixteenth of the codes' (as of two arrays allocated alike).  ctx_len: int32 [batch] on
+    the GPU.  dtype: of the queries, draft rows, summaries and outputs that go with it."""
+
+    def __init__(self, k, v, k_scale, v_scale, ctx_len, block_size, max_blocks=None, layout="bhtd", dtype=torch.bfloat16):
+        if dtype not in _DTYPE:
+            raise ValueError("dtype: float32 or bfloat16")
+        if any(t.dtype != torch.uint8 or t.dim() != 4 for t in (k, v, k_scale, v_scale)) or k.shape != v.shape or k_scale.shape != v_scale.shape:
+            raise ValueError("codes and scales: uint8, 4-d, k and v of one shape each")
+        if any(not t.is_cuda for t in (k, v, k_scale, v_scale)):
+            raise ValueError("codes and scales must live on the GPU")
+        if tuple(k_scale.shape[:3]) != tuple(k.shape[:3]) or k.shape[3] != 16 * k_scale.shape[3]:
+            raise ValueError("scales: one byte to 16 bytes of codes")
+        if k.stride() != v.stride() or k.stride(3) != 1 or k_scale.stride() != v_scale.stride() or k_scale.stride(3) != 1 \
+                or any(k.stride(i) != 16 * k_scale.stride(i) and k.shape[i] > 1 for i in range(3)):
+            raise ValueError("k and v must share strides, the scales' a sixteenth of them; rows must be contiguous")
+        if layout == "bhtd":
+            batch, hkv, T, half = k.shape
+            sb, sh, st = k.stride(0), k.stride(1), k.stride(2)
+        elif layout == "bthd":
+            batch, T, hkv, half = k.shape
+            sb, st, sh = k.stride(0), k.stride(1), k.stride(2)
+        else:
+            raise ValueError(layout)
+        self.k, self.v, self.k_scale, self.v_scale, self.ctx_len = k, v, k_scale, v_scale, ctx_len
+        self.batch, self.Hkv, self.T, self.D, self.B = batch, hkv, T, 2 * half, int(block_size)
+        self.max_blocks = int(max_blocks) if max_blocks is not None else (T + self.B - 1) // self.B
+        if self.max_blocks * self.B > T + self.B - 1:
+            raise ValueError("max_blocks exceeds the allocated rows")
+        if ctx_len.dtype != torch.int32 or ctx_len.numel() != batch:
+            raise ValueError("ctx_len: int32 [batch]")
+        self.dtype = dtype
+        self.c = _PackedKV(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), sb, sh, st,
+                           _ptr(ctx_len, torch.int32, "ctx_len").value, batch, hkv, self.D, self.B, self.max_blocks, _DTYPE[dtype])
 
     def summary_shape(self):
         return (self.batch, self.Hkv, self.max_blocks, self.D)
@@ -476,6 +545,142 @@ def specpv_commit_accepted_layers(kvs, buf_ks, buf_vs, pending_cap, M_tree, n_pe
                                                 _ptr(accepted, torch.int32, "accepted"),
                                                 _ptr(n_accepted, torch.int32, "n_accepted"), int(accepted.shape[1]),
                                                 int(mode), km, kn, ls, _dropped(kv0, dropped), wp, wb, _stream()))
+
+
+def _per_sequence(kv, t, name):
+    if t is not None and tuple(t.shape) != (kv.batch,):
+        raise ValueError("%s: int32 [batch]" % name)
+    return _ptr(t, torch.int32, name)
+
+
+def _sel_or_none(kv, sel_idx, sel_count):
+    if sel_idx is None:
+        if sel_count is not None:
+            raise ValueError("sel_count without sel_idx")
+        return None, None, 0
+    n_sel = sel_idx.shape[-1]
+    _check_sel(kv, sel_idx, sel_count, n_sel)
+    return _ptr(sel_idx, torch.int32, "sel_idx"), _ptr(sel_count, torch.int32, "sel_count"), n_sel
+
+
+def specpv_pack_tokens(kv, packed, dst_begin=None, src_begin=None, src_rows=None, n_rows=None, max_rows=None, kmax=None, kmin=None):
+    """Rows of the KV `kv` into the PackedKV `packed` from token dst_begin[b] on: rows src_rows[b, i] (int32 [batch, n]), or
+    src_begin[b] + i; n_rows[b] of them (default: all of src_rows, or up to kv.ctx_len[b]).  max_rows: the most that any
+    sequence has (default: the width of src_rows, or all that `packed` has room for).  kmax, kmin: the summaries of packed's blocks."""
+    if max_rows is None:
+        max_rows = src_rows.shape[1] if src_rows is not None else packed.max_blocks * packed.B
+    rc = (_native or _loaded()).pack(kv, packed, dst_begin, src_begin, src_rows, n_rows, max_rows, kmax, kmin)
+    if rc is not None:
+        return _check(rc)
+    if (kv.batch, kv.Hkv, kv.D, kv.dtype) != (packed.batch, packed.Hkv, packed.D, packed.dtype):
+        raise ValueError("kv and packed disagree in batch, heads, head dim or dtype")
+    if src_rows is not None and (src_rows.dim() != 2 or tuple(src_rows.shape) != (packed.batch, int(max_rows))):
+        raise ValueError("src_rows: int32 [batch, max_rows]")
+    if (kmax is None) != (kmin is None):
+        raise ValueError("kmax, kmin: both or neither")
+    for name, t in (("kmax", kmax), ("kmin", kmin)):
+        if t is not None and tuple(t.shape) != packed.summary_shape():
+            raise ValueError("%s: [batch, Hkv, max_blocks, D]" % name)
+    _check(load().specpv_pack_tokens(ctypes.byref(kv.c), _per_sequence(packed, src_begin, "src_begin"), _ptr(src_rows, torch.int32, "src_rows"),
+                                     _per_sequence(packed, n_rows, "n_rows"), int(max_rows), ctypes.byref(packed.c),
+                                     _per_sequence(packed, dst_begin, "dst_begin"), _ptr(kmax, packed.dtype, "kmax"),
+                                     _ptr(kmin, packed.dtype, "kmin"), _stream()))
+
+
+def specpv_packed_workspace_bytes(packed, tree=None, cfg=None):
+    return int(load().specpv_packed_workspace_bytes(ctypes.byref(packed.c), None if tree is None else ctypes.byref(tree.c),
+                                                    None if cfg is None else ctypes.byref(cfg.c)))
+
+
+def specpv_packed_select_blocks(packed, tree, kmax, kmin, cfg, sel_idx, sel_count, scores=None, workspace=None):
+    """specpv_select_blocks for a cache in 4 bits."""
+    rc = (_native or _loaded()).packed_select(packed, tree, kmax, kmin, cfg, sel_idx, sel_count, scores, workspace)
+    if rc is not None:
+        return _check(rc)
+    _match(packed, tree)
+    _check_sel(packed, sel_idx, sel_count, cfg.n_sel)
+    if scores is not None and tuple(scores.shape) != (packed.batch, packed.Hkv, packed.max_blocks):
+        raise ValueError("scores: [batch, Hkv, max_blocks] float32")
+    for name, t in (("kmax", kmax), ("kmin", kmin)):
+        if tuple(t.shape) != packed.summary_shape():
+            raise ValueError("%s: [batch, Hkv, max_blocks, D]" % name)
+    wp, wb = _ws(workspace)
+    _check(load().specpv_packed_select_blocks(ctypes.byref(packed.c), ctypes.byref(tree.c), _ptr(kmax, packed.dtype, "kmax"),
+                                              _ptr(kmin, packed.dtype, "kmin"), ctypes.byref(cfg.c),
+                                              _ptr(sel_idx, torch.int32, "sel_idx"), _ptr(sel_count, torch.int32, "sel_count"),
+                                              _ptr(scores, torch.float32, "scores"), wp, wb, _stream()))
+
+
+def specpv_packed_verify_attn(packed, tree, sel_idx, sel_count, out, lse=None, workspace=None):
+    """specpv_partial_verify_attn over a cache in 4 bits (sel_idx None: over all of it)."""
+    rc = (_native or _loaded()).packed_attn(packed, tree, sel_idx, sel_count, out, lse, workspace)
+    if rc is not None:
+        return _check(rc)
+    _match(packed, tree)
+    si, sc, n_sel = _sel_or_none(packed, sel_idx, sel_count)
+    if out.shape != tree.q.shape:
+        raise ValueError("out: same shape as q")
+    if lse is not None and tuple(lse.shape) != (tree.batch, tree.Mq, tree.Hq):
+        raise ValueError("lse: [batch, Mq, Hq] float32")
+    wp, wb = _ws(workspace)
+    _check(load().specpv_packed_verify_attn(ctypes.byref(packed.c), ctypes.byref(tree.c), si, sc, n_sel, _ptr(out, packed.dtype, "out"),
+                                            _ptr(lse, torch.float32, "lse"), wp, wb, _stream()))
+
+
+def specpv_packed_gather_blocks(packed, sel_idx, sel_count, out_k, out_v, out_len=None):
+    """Kept blocks (sel_idx None: all) of a cache in 4 bits as rows of its dtype: out_k / out_v [batch, Hkv, n_sel * B, D]
+    (all: [batch, Hkv, max_blocks * B, D]); out_len int32 [batch] (optional)."""
+    rc = (_native or _loaded()).packed_gather(packed, sel_idx, sel_count, out_k, out_v, out_len)
+    if rc is not None:
+        return _check(rc)
+    si, sc, n_sel = _sel_or_none(packed, sel_idx, sel_count)
+    for name, t in (("out_k", out_k), ("out_v", out_v)):
+        if tuple(t.shape) != (packed.batch, packed.Hkv, (n_sel if sel_idx is not None else packed.max_blocks) * packed.B, packed.D):
+            raise ValueError("%s: [batch, Hkv, blocks * B, D]" % name)
+    _check(load().specpv_packed_gather_blocks(ctypes.byref(packed.c), si, sc, n_sel, _ptr(out_k, packed.dtype, "out_k"),
+                                              _ptr(out_v, packed.dtype, "out_v"), _per_sequence(packed, out_len, "out_len"), _stream()))
+
+
+def specpv_accumulate_weights(kv, tree, lse, weights, nodes=None, n_nodes=None, sel_idx=None, sel_count=None):
+    """weights [batch, Hkv, max_blocks * B] float32 += the attention weight of each cached token over the query rows `nodes`
+    (int32 [batch, n], n_nodes [batch] of them; None: all) of a pass whose log-sum-exp is lse [batch, Mq, Hq]."""
+    rc = (_native or _loaded()).weigh(kv, tree, lse, weights, nodes, n_nodes, sel_idx, sel_count)
+    if rc is not None:
+        return _check(rc)
+    _match(kv, tree)
+    if tuple(lse.shape) != (tree.batch, tree.Mq, tree.Hq):
+        raise ValueError("lse: [batch, Mq, Hq] float32")
+    if tuple(weights.shape) != (kv.batch, kv.Hkv, kv.max_blocks * kv.B):
+        raise ValueError("weights: [batch, Hkv, max_blocks * B] float32")
+    if (nodes is None) != (n_nodes is None) or (nodes is not None and (nodes.dim() != 2 or nodes.shape[0] != kv.batch)):
+        raise ValueError("nodes: int32 [batch, n] with n_nodes: int32 [batch]")
+    si, sc, n_sel = _sel_or_none(kv, sel_idx, sel_count)
+    _check(load().specpv_accumulate_weights(ctypes.byref(kv.c), ctypes.byref(tree.c), _ptr(lse, torch.float32, "lse"), _ptr(nodes, torch.int32, "nodes"),
+                                            _per_sequence(kv, n_nodes, "n_nodes"), 0 if nodes is None else int(nodes.shape[1]), si, sc, n_sel,
+                                            _ptr(weights, torch.float32, "weights"), _stream()))
+
+
+def specpv_evict_workspace_bytes(kv):
+    return int(load().specpv_evict_workspace_bytes(ctypes.byref(kv.c)))
+
+
+def specpv_evict_tokens(kv, weights, n_sink, n_recent, k_tokens, dst, keep_idx, dst_weights=None, workspace=None):
+    """The first n_sink, the last n_recent and the k_tokens heaviest of the other tokens of every KV head into the KV `dst`,
+    whose ctx_len is written; keep_idx int32 [batch, Hkv, n_sink + k_tokens + n_recent]; dst_weights: their weights."""
+    rc = (_native or _loaded()).evict(kv, weights, n_sink, n_recent, k_tokens, dst, keep_idx, dst_weights, workspace)
+    if rc is not None:
+        return _check(rc)
+    if (kv.batch, kv.Hkv, kv.D, kv.dtype) != (dst.batch, dst.Hkv, dst.D, dst.dtype):
+        raise ValueError("kv and dst disagree in batch, heads, head dim or dtype")
+    for name, t, c in (("weights", weights, kv), ("dst_weights", dst_weights, dst)):
+        if t is not None and tuple(t.shape) != (c.batch, c.Hkv, c.max_blocks * c.B):
+            raise ValueError("%s: [batch, Hkv, max_blocks * B] float32" % name)
+    if tuple(keep_idx.shape) != (kv.batch, kv.Hkv, int(n_sink) + int(n_recent) + int(k_tokens)):
+        raise ValueError("keep_idx: int32 [batch, Hkv, n_sink + k_tokens + n_recent]")
+    wp, wb = _ws(workspace)
+    _check(load().specpv_evict_tokens(ctypes.byref(kv.c), _ptr(weights, torch.float32, "weights"), int(n_sink), int(n_recent), int(k_tokens),
+                                      ctypes.byref(dst.c), _ptr(dst_weights, torch.float32, "dst_weights"), _ptr(keep_idx, torch.int32, "keep_idx"),
+                                      wp, wb, _stream()))
 
 
 def specpv_debug_set_timeline(buf):

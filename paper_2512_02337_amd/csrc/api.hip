@@ -5,7 +5,7 @@
 #include <stdio.h>
 #include <string.h>
 
-#include "internal.h"
+#include "packed.h"
 
 namespace specpv {
 
@@ -625,6 +625,54 @@ static int run_select(const Shape &s, int dtype, const specpv_tree *tree, const 
     return SPECPV_OK;
 }
 
+// ---- the cache in 4 bits ----
+
+static int check_packed(const specpv_packed_kv *kv)
+{
+    if (!kv || !kv->k || !kv->v || !kv->k_scale || !kv->v_scale || !kv->ctx_len) return SPECPV_EINVAL;
+    if (kv->dtype != SPECPV_F32 && kv->dtype != SPECPV_BF16) return SPECPV_EINVAL;
+    if (kv->head_dim != 64 && kv->head_dim != 128) return SPECPV_EINVAL;
+    if (kv->batch < 1 || kv->n_kv_heads < 1 || kv->block_size < 1 || kv->max_blocks < 1) return SPECPV_EINVAL;
+    const int64_t row = kv->head_dim / 2;
+    if (kv->stride_t < row || kv->stride_t % row || kv->stride_h % row || kv->stride_b % row || kv->stride_h < 0 || kv->stride_b < 0) return SPECPV_EINVAL;
+    if (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15 || ((uintptr_t)kv->k_scale | (uintptr_t)kv->v_scale) & 3) return SPECPV_EINVAL;
+    if ((int64_t)kv->max_blocks * kv->block_size > ((int64_t)1 << 30)) return SPECPV_ELIMIT;
+    return SPECPV_OK;
+}
+
+// The ordinary descriptor of the same shape, for what reads no rows.
+static specpv_kv kv_of(const specpv_packed_kv *p)
+{
+    return specpv_kv{p->k, p->v, p->stride_b, p->stride_h, p->stride_t, p->ctx_len, p->batch, p->n_kv_heads, p->head_dim, p->block_size, p->max_blocks, p->dtype};
+}
+
+static PackedShape make_packed(const specpv_packed_kv *p, const specpv_tree *tree)
+{
+    const specpv_kv kv = kv_of(p);
+    return PackedShape{make_shape(&kv, tree), (const uint8_t *)p->k_scale, (const uint8_t *)p->v_scale};
+}
+
+// fp16 partials (bf16 at 128 channels), where the tree has no nodes that are keys only: those are the combine's here, which takes
+// fp32 ones with them.
+static bool packed_half(const Shape &s, int dtype) { return dtype == SPECPV_BF16 && s.D == 128 && s.koff == 0; }
+static size_t packed_row_bytes(const Shape &s, int dtype) { return (size_t)s.D * (packed_half(s, dtype) ? 2 : 4); }
+static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
+{
+    const size_t rows = (size_t)s.batch * s.Hq * nsplit * s.M;
+    return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
+}
+
+// Splits: two workgroups of four wavefronts a CU.
+static int64_t packed_splits(const Shape &s, int64_t n_blocks)
+{
+    const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
+    const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s);
+    int64_t ns = (2 * (int64_t)device_cu_count() + columns - 1) / columns;
+    if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
+    if (ns > 128) ns = 128;
+    return ns < 1 ? 1 : ns;
+}
+
 }  // namespace specpv
 
 using namespace specpv;
@@ -882,6 +930,123 @@ int specpv_commit_accepted_layers(const specpv_kv *const *kv, void *const *buf_k
     return e == hipSuccess ? SPECPV_OK : fail_hip(e);
 }
 
+int specpv_pack_tokens(const specpv_kv *src, const int32_t *src_begin, const int32_t *src_rows, const int32_t *n_rows, int32_t max_rows,
+                       const specpv_packed_kv *dst, const int32_t *dst_begin, void *kmax, void *kmin, void *stream)
+{
+    int rc = check_kv(src);
+    if (rc != SPECPV_OK || (rc = check_packed(dst)) != SPECPV_OK) return rc;
+    if (src->batch != dst->batch || src->n_kv_heads != dst->n_kv_heads || src->head_dim != dst->head_dim || src->dtype != dst->dtype) return SPECPV_EINVAL;
+    if (max_rows < 1 || (src_rows && src_begin)) return SPECPV_EINVAL;
+    if ((kmax == nullptr) != (kmin == nullptr) || ((uintptr_t)kmax | (uintptr_t)kmin) & 15) return SPECPV_EINVAL;
+    if (dst->batch > 65535 || dst->n_kv_heads > 65535) return SPECPV_ELIMIT;
+    const PackArgs a{src_begin, src_rows, n_rows, dst_begin, max_rows, kmax, kmin};
+    const hipError_t e = launch_pack(make_shape(src, nullptr), src->dtype, make_packed(dst, nullptr), a, (hipStream_t)stream);
+    return e == hipSuccess ? SPECPV_OK : fail_hip(e);
+}
+
+size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tree *tree, const specpv_select_cfg *cfg)
+{
+    if (check_packed(kv) != SPECPV_OK) return 0;
+    const specpv_kv plain = kv_of(kv);
+    if (!tree) return kArriveBytes + 256;
+    if (check_tree(&plain, tree, false) != SPECPV_OK) return 0;
+    const Shape s = make_shape(&plain, tree);
+    size_t need = packed_bytes(s, kv->dtype, packed_splits(s, s.max_blocks));
+    if (cfg) {
+        const int64_t n_sel = (int64_t)cfg->n_sink_blocks + cfg->k_blocks + cfg->n_recent_blocks + cfg->n_extra_slots;
+        const size_t lists = packed_bytes(s, kv->dtype, packed_splits(s, n_sel)), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
+        if (lists > need) need = lists;
+        if (scores > need) need = scores;
+    }
+    return need;
+}
+
+int specpv_packed_select_blocks(const specpv_packed_kv *kv, const specpv_tree *tree, const void *kmax, const void *kmin,
+                                const specpv_select_cfg *cfg, int32_t *sel_idx, int32_t *sel_count, float *scores,
+                                void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = check_packed(kv);
+    if (rc != SPECPV_OK) return rc;
+    specpv_kv plain = kv_of(kv);
+    plain.stride_b = plain.stride_h = 0;   // (no row is read)
+    plain.stride_t = kv->head_dim;
+    return specpv_select_blocks(&plain, tree, kmax, kmin, cfg, sel_idx, sel_count, scores, workspace, workspace_bytes, stream);
+}
+
+int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tree, const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel,
+                              void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_packed(kv);
+    if (rc != SPECPV_OK) return rc;
+    const specpv_kv plain = kv_of(kv);
+    if ((rc = check_tree(&plain, tree, true)) != SPECPV_OK) return rc;
+    if (!out || ((uintptr_t)out & 15)) return SPECPV_EINVAL;
+    if (sel_idx && (!sel_count || n_sel < 0)) return SPECPV_EINVAL;
+    if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
+    const PackedShape p = make_packed(kv, tree);
+    const Shape &s = p.s;
+    if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, 1)) return SPECPV_EWORKSPACE;
+    int64_t ns = packed_splits(s, sel_idx ? n_sel : s.max_blocks);
+    while (ns > 1 && packed_bytes(s, kv->dtype, ns) > workspace_bytes) --ns;
+    if ((int64_t)packed_row_tiles(s) * ns > 65535) return SPECPV_ELIMIT;
+    const size_t rows = (size_t)s.batch * s.Hq * ns * s.M;
+    char *const at = (char *)workspace + kArriveBytes;
+    const Partials part{(float *)at, (float *)(at + align_up(rows * packed_row_bytes(s, kv->dtype))), (int)ns, packed_half(s, kv->dtype) ? 1 : 0, 0, nullptr};
+    hipError_t e = launch_packed_attn(p, kv->dtype, sel_idx, sel_count, n_sel, part, (hipStream_t)stream);
+    if (e == hipSuccess) e = launch_combine(s, kv->dtype, part, out, lse, (hipStream_t)stream);
+    return e == hipSuccess ? SPECPV_OK : fail_hip(e);
+}
+
+int specpv_packed_gather_blocks(const specpv_packed_kv *kv, const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel,
+                                void *out_k, void *out_v, int32_t *out_len, void *stream)
+{
+    const int rc = check_packed(kv);
+    if (rc != SPECPV_OK) return rc;
+    if (!out_k || !out_v || (sel_idx && (!sel_count || n_sel < 1))) return SPECPV_EINVAL;
+    if (((uintptr_t)out_k | (uintptr_t)out_v) & 15) return SPECPV_EINVAL;
+    if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
+    if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
+    const hipError_t e = launch_packed_gather(make_packed(kv, nullptr), kv->dtype, sel_idx, sel_count, n_sel, out_k, out_v, out_len, (hipStream_t)stream);
+    return e == hipSuccess ? SPECPV_OK : fail_hip(e);
+}
+
+int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, const float *lse, const int32_t *nodes, const int32_t *n_nodes,
+                              int32_t max_nodes, const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel, float *weights, void *stream)
+{
+    int rc = check_kv(kv);
+    if (rc != SPECPV_OK) return rc;
+    if ((rc = check_tree(kv, tree, false)) != SPECPV_OK) return rc;
+    if (!lse || !weights || (nodes && (!n_nodes || max_nodes < 1)) || (sel_idx && (!sel_count || n_sel < 0))) return SPECPV_EINVAL;
+    if (nodes && max_nodes > SPECPV_MAX_M) return SPECPV_ELIMIT;
+    if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
+    if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
+    const Shape s = make_shape(kv, tree);
+    const hipError_t e = launch_weigh(s, kv->dtype, WeighArgs{lse, nodes, n_nodes, max_nodes, sel_idx, sel_count, n_sel, weights}, (hipStream_t)stream);
+    return e == hipSuccess ? SPECPV_OK : fail_hip(e);
+}
+
+size_t specpv_evict_workspace_bytes(const specpv_kv *kv)
+{
+    return check_kv(kv) == SPECPV_OK ? kArriveBytes + align_up(evict_scratch_bytes((int64_t)kv->batch * kv->n_kv_heads)) : 0;
+}
+
+int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sink, int32_t n_recent, int32_t k_tokens, const specpv_kv *dst,
+                        float *dst_weights, int32_t *keep_idx, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_kv(kv);
+    if (rc != SPECPV_OK || (rc = check_kv(dst)) != SPECPV_OK) return rc;
+    if (kv->batch != dst->batch || kv->n_kv_heads != dst->n_kv_heads || kv->head_dim != dst->head_dim || kv->dtype != dst->dtype) return SPECPV_EINVAL;
+    if (!weights || !keep_idx || n_sink < 0 || n_recent < 0 || k_tokens < 0) return SPECPV_EINVAL;
+    if (kv->k == dst->k || kv->v == dst->v || kv->ctx_len == dst->ctx_len || weights == dst_weights) return SPECPV_EINVAL;
+    const int64_t n = (int64_t)n_sink + n_recent + k_tokens;
+    if (n < 1 || n > (int64_t)dst->max_blocks * dst->block_size) return SPECPV_EINVAL;
+    if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
+    if (!workspace || workspace_bytes < specpv_evict_workspace_bytes(kv)) return SPECPV_EWORKSPACE;
+    const EvictArgs a{n_sink, n_recent, k_tokens, weights, dst_weights, keep_idx, (uint32_t *)workspace, (uint32_t *)((char *)workspace + kArriveBytes)};
+    const hipError_t e = launch_evict(make_shape(kv, nullptr), make_shape(dst, nullptr), kv->dtype, a, (hipStream_t)stream);
+    return e == hipSuccess ? SPECPV_OK : fail_hip(e);
+}
+
 const char *specpv_strerror(int status)
 {
     switch (status) {
@@ -919,6 +1084,6 @@ int specpv_debug_set_select_route(int route)
     return SPECPV_OK;
 }
 
-int specpv_version(void) { return 202; }
+int specpv_version(void) { return 203; }
 
 }  // extern "C"

@@ -18,7 +18,7 @@
 
 namespace {
 
-enum Fn { kSummarize, kSelect, kPartial, kPartialStatic, kRefresh, kGather, kCommit, kCommitLayers, kFns };
+enum Fn { kSummarize, kSelect, kPartial, kPartialStatic, kRefresh, kGather, kCommit, kCommitLayers, kPack, kPackedSelect, kPackedAttn, kPackedGather, kWeigh, kEvict, kFns };
 void *g_fn[kFns];
 PyObject *s_c, *s_q, *s_kd;
 
@@ -51,7 +51,7 @@ private:
     const S *p_ = nullptr;
 };
 
-at::ScalarType scalar(const specpv_kv *kv) { return kv->dtype == SPECPV_BF16 ? at::kBFloat16 : at::kFloat; }
+template <typename KV> at::ScalarType scalar(const KV *kv) { return kv->dtype == SPECPV_BF16 ? at::kBFloat16 : at::kFloat; }
 
 // A contiguous GPU tensor of this type and shape.
 bool tensor(PyObject *o, at::ScalarType dt, std::initializer_list<int64_t> shape, void **out)
@@ -110,7 +110,7 @@ struct Ref {
     Ref &operator=(const Ref &) = delete;
 };
 // kv and tree belong together (binding.py: _match)
-bool match(const Desc<specpv_kv> &kv, PyObject *tree_obj, const Desc<specpv_tree> &tree)
+template <typename KV> bool match(const Desc<KV> &kv, PyObject *tree_obj, const Desc<specpv_tree> &tree)
 {
     if (!kv || !tree) return false;
     const Ref q(PyObject_GetAttr(tree_obj, s_q)), kd(PyObject_GetAttr(tree_obj, s_kd));
@@ -120,11 +120,11 @@ bool match(const Desc<specpv_kv> &kv, PyObject *tree_obj, const Desc<specpv_tree
     if (PyErr_Occurred()) PyErr_Clear();
     return ok;
 }
-bool lists(const specpv_kv *kv, PyObject *idx, PyObject *cnt, int64_t n_sel, void **pi, void **pc)
+template <typename KV> bool lists(const KV *kv, PyObject *idx, PyObject *cnt, int64_t n_sel, void **pi, void **pc)
 {
     return tensor(idx, at::kInt, {kv->batch, kv->n_kv_heads, n_sel}, pi) && tensor(cnt, at::kInt, {kv->batch, kv->n_kv_heads}, pc);
 }
-bool summaries(const specpv_kv *kv, PyObject *kmax, PyObject *kmin, void **px, void **pn)
+template <typename KV> bool summaries(const KV *kv, PyObject *kmax, PyObject *kmin, void **px, void **pn)
 {
     return tensor(kmax, scalar(kv), {kv->batch, kv->n_kv_heads, kv->max_blocks, kv->head_dim}, px) &&
            tensor(kmin, scalar(kv), {kv->batch, kv->n_kv_heads, kv->max_blocks, kv->head_dim}, pn);
@@ -359,6 +359,140 @@ PyObject *commit(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// An int32 tensor of the sequences, or None.
+template <typename KV> bool per_sequence(const KV *kv, PyObject *o, void **out) { return tensor_or_none(o, at::kInt, {kv->batch}, out); }
+// Lists, or None for both.
+template <typename KV> bool lists_or_none(const KV *kv, PyObject *idx, PyObject *cnt, int64_t *n_sel, void **pi, void **pc)
+{
+    *pi = *pc = nullptr;
+    *n_sel = 0;
+    if (idx == Py_None) return cnt == Py_None;
+    return last_extent(idx, n_sel) && *n_sel <= INT32_MAX && lists(kv, idx, cnt, *n_sel, pi, pc);
+}
+// The second extent of [batch, n] int32, its address; None: 0 and nothing.
+template <typename KV> bool row_lists(const KV *kv, PyObject *o, int64_t *n, void **out)
+{
+    *out = nullptr;
+    *n = 0;
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.dim() != 2 || t.size(1) > INT32_MAX) return false;
+    *n = t.size(1);
+    return tensor(o, at::kInt, {kv->batch, *n}, out);
+}
+
+PyObject *pack(PyObject *, PyObject *const *a, Py_ssize_t n)   // kv, packed, dst_begin, src_begin, src_rows, n_rows, max_rows, kmax, kmin
+{
+    SPECPV_ARGS(9);
+    Desc<specpv_kv> kv(a[0]);
+    Desc<specpv_packed_kv> to(a[1]);
+    if (!kv || !to || kv->batch != to->batch || kv->n_kv_heads != to->n_kv_heads || kv->head_dim != to->head_dim || kv->dtype != to->dtype) Py_RETURN_NONE;
+    void *db, *sb, *sr, *nr, *kx = nullptr, *kn = nullptr;
+    int64_t width;
+    int32_t most;
+    if (!per_sequence(to.get(), a[2], &db) || !per_sequence(to.get(), a[3], &sb) || !row_lists(to.get(), a[4], &width, &sr) || !per_sequence(to.get(), a[5], &nr) ||
+        !integer(a[6], &most) || (sr && most != width))
+        Py_RETURN_NONE;
+    if (a[7] != Py_None || a[8] != Py_None) {
+        if (!summaries(to.get(), a[7], a[8], &kx, &kn)) Py_RETURN_NONE;
+    }
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_pack_tokens)>(kPack)(kv.get(), (int32_t *)sb, (int32_t *)sr, (int32_t *)nr, most, to.get(), (int32_t *)db, kx, kn, st);
+    });
+}
+
+PyObject *packed_select(PyObject *, PyObject *const *a, Py_ssize_t n)   // as select
+{
+    SPECPV_ARGS(9);
+    Desc<specpv_packed_kv> kv(a[0]);
+    Desc<specpv_tree> tree(a[1]);
+    Desc<specpv_select_cfg> cfg(a[4]);
+    void *kx, *kn, *si, *sc, *so, *ws;
+    size_t wb;
+    if (!cfg || !match(kv, a[1], tree) || !summaries(kv.get(), a[2], a[3], &kx, &kn) || !lists(kv.get(), a[5], a[6], row_entries(cfg.get()), &si, &sc) ||
+        !tensor_or_none(a[7], at::kFloat, {kv->batch, kv->n_kv_heads, kv->max_blocks}, &so) || !workspace(a[8], &ws, &wb))
+        Py_RETURN_NONE;
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_packed_select_blocks)>(kPackedSelect)(kv.get(), tree.get(), kx, kn, cfg.get(), (int32_t *)si, (int32_t *)sc, (float *)so, ws, wb, st);
+    });
+}
+
+PyObject *packed_attn(PyObject *, PyObject *const *a, Py_ssize_t n)   // kv, tree, sel_idx, sel_count, out, lse, workspace
+{
+    SPECPV_ARGS(7);
+    Desc<specpv_packed_kv> kv(a[0]);
+    Desc<specpv_tree> tree(a[1]);
+    if (!match(kv, a[1], tree)) Py_RETURN_NONE;
+    const int64_t Mq = tree->M - tree->n_key_only;
+    void *si, *sc, *out, *lse, *ws;
+    size_t wb;
+    int64_t n_sel;
+    if (!lists_or_none(kv.get(), a[2], a[3], &n_sel, &si, &sc) || !tensor(a[4], scalar(kv.get()), {kv->batch, Mq, tree->n_q_heads, kv->head_dim}, &out) ||
+        !tensor_or_none(a[5], at::kFloat, {kv->batch, Mq, tree->n_q_heads}, &lse) || !workspace(a[6], &ws, &wb))
+        Py_RETURN_NONE;
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_packed_verify_attn)>(kPackedAttn)(kv.get(), tree.get(), (int32_t *)si, (int32_t *)sc, (int32_t)n_sel, out, (float *)lse, ws, wb, st);
+    });
+}
+
+PyObject *packed_gather(PyObject *, PyObject *const *a, Py_ssize_t n)   // kv, sel_idx, sel_count, out_k, out_v, out_len
+{
+    SPECPV_ARGS(6);
+    Desc<specpv_packed_kv> kv(a[0]);
+    int64_t n_sel;
+    void *si, *sc, *ok, *ov, *ol;
+    if (!kv || !lists_or_none(kv.get(), a[1], a[2], &n_sel, &si, &sc)) Py_RETURN_NONE;
+    const int64_t rows = (si ? n_sel : (int64_t)kv->max_blocks) * kv->block_size;
+    if (!tensor(a[3], scalar(kv.get()), {kv->batch, kv->n_kv_heads, rows, kv->head_dim}, &ok) ||
+        !tensor(a[4], scalar(kv.get()), {kv->batch, kv->n_kv_heads, rows, kv->head_dim}, &ov) || !per_sequence(kv.get(), a[5], &ol))
+        Py_RETURN_NONE;
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_packed_gather_blocks)>(kPackedGather)(kv.get(), (int32_t *)si, (int32_t *)sc, (int32_t)n_sel, ok, ov, (int32_t *)ol, st);
+    });
+}
+
+PyObject *weigh(PyObject *, PyObject *const *a, Py_ssize_t n)   // kv, tree, lse, weights, nodes, n_nodes, sel_idx, sel_count
+{
+    SPECPV_ARGS(8);
+    Desc<specpv_kv> kv(a[0]);
+    Desc<specpv_tree> tree(a[1]);
+    if (!match(kv, a[1], tree)) Py_RETURN_NONE;
+    void *lse, *w, *nd, *nn, *si, *sc;
+    int64_t n_sel, most;
+    if (!tensor(a[2], at::kFloat, {kv->batch, tree->M - tree->n_key_only, tree->n_q_heads}, &lse) ||
+        !tensor(a[3], at::kFloat, {kv->batch, kv->n_kv_heads, (int64_t)kv->max_blocks * kv->block_size}, &w) || !row_lists(kv.get(), a[4], &most, &nd) ||
+        !per_sequence(kv.get(), a[5], &nn) || (nd == nullptr) != (nn == nullptr) || !lists_or_none(kv.get(), a[6], a[7], &n_sel, &si, &sc))
+        Py_RETURN_NONE;
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_accumulate_weights)>(kWeigh)(kv.get(), tree.get(), (float *)lse, (int32_t *)nd, (int32_t *)nn, (int32_t)most, (int32_t *)si,
+                                                               (int32_t *)sc, (int32_t)n_sel, (float *)w, st);
+    });
+}
+
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n)   // kv, weights, n_sink, n_recent, k_tokens, dst, keep_idx, dst_weights, workspace
+{
+    SPECPV_ARGS(9);
+    Desc<specpv_kv> kv(a[0]), to(a[5]);
+    int32_t ns, nr, k;
+    void *w, *nw, *ki, *ws;
+    size_t wb;
+    if (!kv || !to || kv->batch != to->batch || kv->n_kv_heads != to->n_kv_heads || kv->head_dim != to->head_dim || kv->dtype != to->dtype || !integer(a[2], &ns) || !integer(a[3], &nr) || !integer(a[4], &k) ||
+        !tensor(a[1], at::kFloat, {kv->batch, kv->n_kv_heads, (int64_t)kv->max_blocks * kv->block_size}, &w) ||
+        !tensor(a[6], at::kInt, {kv->batch, kv->n_kv_heads, (int64_t)ns + nr + k}, &ki) ||
+        !tensor_or_none(a[7], at::kFloat, {to->batch, to->n_kv_heads, (int64_t)to->max_blocks * to->block_size}, &nw) || !workspace(a[8], &ws, &wb))
+        Py_RETURN_NONE;
+    void *st = stream();
+    return enter([&] {
+        return fn<decltype(&specpv_evict_tokens)>(kEvict)(kv.get(), (float *)w, ns, nr, k, to.get(), (float *)nw, (int32_t *)ki, ws, wb, st);
+    });
+}
+
 PyObject *set_table(PyObject *, PyObject *const *a, Py_ssize_t n)   // the addresses of the library's functions, in the order of Fn
 {
     if (n != kFns) {
@@ -375,7 +509,8 @@ PyObject *set_table(PyObject *, PyObject *const *a, Py_ssize_t n)   // the addre
 
 #define SPECPV_METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))guarded<NAME>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SPECPV_METHOD(set_table), SPECPV_METHOD(summarize), SPECPV_METHOD(select),        SPECPV_METHOD(partial), SPECPV_METHOD(partial_static),
-                         SPECPV_METHOD(refresh),   SPECPV_METHOD(gather),    SPECPV_METHOD(commit_layers), SPECPV_METHOD(commit),  {nullptr, nullptr, 0, nullptr}};
+                         SPECPV_METHOD(refresh),   SPECPV_METHOD(gather),    SPECPV_METHOD(commit_layers), SPECPV_METHOD(commit),
+                         SPECPV_METHOD(pack),      SPECPV_METHOD(packed_select), SPECPV_METHOD(packed_attn), SPECPV_METHOD(packed_gather), SPECPV_METHOD(weigh), SPECPV_METHOD(evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "The calls of binding.py without the Python work per call.", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

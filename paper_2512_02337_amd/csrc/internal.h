@@ -334,6 +334,28 @@ hipError_t launch_commit(const Shape &s, int dtype, int n_layers, void *const *k
 hipError_t launch_gather(const Shape &s, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel,
                          void *out_k, void *out_v, int32_t *out_len, hipStream_t st);
 
+// Accumulated attention weights (weights.hip): query rows of `nodes` [batch, max_nodes] (n_nodes of them), or of every node.
+struct WeighArgs {
+    const float *lse;                    // [batch, M, Hq]
+    const int32_t *nodes, *n_nodes;
+    int max_nodes;
+    const int32_t *sel_idx, *sel_count;
+    int n_sel;
+    float *weights;                      // [batch, Hkv, max_blocks * B]
+};
+hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream_t st);
+
+// Eviction by accumulated weight (evict.hip): ns + k + nr tokens of each (sequence, KV head) of `s` go to `d`, whose lengths are written.
+struct EvictArgs {
+    int ns, nr, k;
+    const float *weights;      // [batch, Hkv, tokens that s has room for]
+    float *new_weights;        // [batch, Hkv, tokens that d has room for], or nullptr
+    int32_t *keep_idx;         // [batch, Hkv, ns + k + nr]
+    uint32_t *arrive, *scratch;   // a workspace's zeroed words (zero again afterwards), and evict_scratch_bytes of room
+};
+size_t evict_scratch_bytes(int64_t pairs);
+hipError_t launch_evict(const Shape &s, const Shape &d, int dtype, const EvictArgs &a, hipStream_t st);
+
 int device_cu_count();   // of the current device
 
 // One-time set-up per (kernel, device): `fn` runs once for each device it is asked for, also when
