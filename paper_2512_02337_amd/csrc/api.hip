@@ -1027,7 +1027,7 @@ int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, cons
 
 size_t specpv_evict_workspace_bytes(const specpv_kv *kv)
 {
-    return check_kv(kv) == SPECPV_OK ? kArriveBytes + align_up(evict_scratch_bytes((int64_t)kv->batch * kv->n_kv_heads)) : 0;
+    return check_kv(kv) == SPECPV_OK ? kArriveBytes + align_up(evict_scratch_bytes((int64_t)kv->batch * kv->n_kv_heads, (int64_t)kv->max_blocks * kv->block_size)) : 0;
 }
 
 int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sink, int32_t n_recent, int32_t k_tokens, const specpv_kv *dst,
@@ -1042,7 +1042,7 @@ int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sin
     if (n < 1 || n > (int64_t)dst->max_blocks * dst->block_size) return SPECPV_EINVAL;
     if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
     if (!workspace || workspace_bytes < specpv_evict_workspace_bytes(kv)) return SPECPV_EWORKSPACE;
-    const EvictArgs a{n_sink, n_recent, k_tokens, weights, dst_weights, keep_idx, (uint32_t *)workspace, (uint32_t *)((char *)workspace + kArriveBytes)};
+    const EvictArgs a{n_sink, n_recent, k_tokens, weights, dst_weights, keep_idx, (uint32_t *)((char *)workspace + kArriveBytes)};
     const hipError_t e = launch_evict(make_shape(kv, nullptr), make_shape(dst, nullptr), kv->dtype, a, (hipStream_t)stream);
     return e == hipSuccess ? SPECPV_OK : fail_hip(e);
 }

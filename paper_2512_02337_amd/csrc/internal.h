@@ -351,9 +351,9 @@ struct EvictArgs {
     const float *weights;      // [batch, Hkv, tokens that s has room for]
     float *new_weights;        // [batch, Hkv, tokens that d has room for], or nullptr
     int32_t *keep_idx;         // [batch, Hkv, ns + k + nr]
-    uint32_t *arrive, *scratch;   // a workspace's zeroed words (zero again afterwards), and evict_scratch_bytes of room
+    uint32_t *scratch;         // evict_scratch_bytes of room
 };
-size_t evict_scratch_bytes(int64_t pairs);
+size_t evict_scratch_bytes(int64_t pairs, int64_t cap);   // caches of `cap` tokens
 hipError_t launch_evict(const Shape &s, const Shape &d, int dtype, const EvictArgs &a, hipStream_t st);
 
 int device_cu_count();   // of the current device
