@@ -6,35 +6,39 @@
 // A wavefront works for itself: the K codes of a chunk are its A operand as they come from memory (a lane holds half of a
 // token's row; which channels a step of the product takes does not matter as long as Q's are the same), V goes through a
 // piece of LDS of its own as bf16, because its operand has tokens where memory has channels: the transposing LDS reads turn it.
-// The next chunk's codes, 36 bytes a lane, are under way while this one is worked on.
+// The next two chunks' codes, 35 bytes a lane each, are under way while one is worked on.
 #include "packed.h"
-#include <type_traits>
+#include "attn_mfma.h"
 
 namespace specpv {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short i16x4;
 
 struct PackedAttnArgs {
     PackedShape p;
     Partials part;
     const int32_t *sel_idx, *sel_count;
-    int n_sel, row_tiles, pairs;
+    int n_sel, row_tiles;
     FastDiv div_B, div_hkv, div_M, div_tiles;
     float scale_log2;
 };
 
 constexpr int kPackedWaves = 4;
-constexpr float kPackedSlack = 8.f;   // the reference maximum may lag the true one by 2^8
 
 // One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.
 template <typename T> struct Pieces { static constexpr int N = sizeof(T) == 2 ? 1 : 3; };
 
-template <typename T, int D>
+// Which tokens a chunk has.  RUN: they follow each other in memory (the whole cache, or blocks of whole chunks): a scalar row and a
+// count.  Else (blocks of other sizes) a lane looks its token up.
+template <bool RUN> struct ChunkTokens;
+template <> struct ChunkTokens<true> { int row; };
+template <> struct ChunkTokens<false> { int tok; };
+
+template <typename T, int D, bool RUN>
 __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(PackedAttnArgs a)
 {
     constexpr int N = Pieces<T>::N, STEPS = D / 16, GROUPS = D / 32, TILES = D / 32, VLOADS = D / 64;
+    constexpr int RING = N == 1 ? 3 : 2;              // chunks in registers: this one and those under way
     constexpr int VROW = D * 2;                       // bytes of a V row in LDS
     __shared__ __align__(16) char lds[kPackedWaves][32 * VROW];
     __shared__ float2 ml_lds[kPackedWaves][64];
@@ -48,11 +52,8 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     const int64_t cap = (int64_t)s.max_blocks * s.B;
     const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
     const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
-    int cnt = 0, span = L;
-    if (a.sel_idx) {
-        cnt = max(min(a.sel_count[bg], a.n_sel), 0);
-        span = cnt * s.B;
-    }
+    int span = L;
+    if (a.sel_idx) span = L ? max(min(a.sel_count[bg], a.n_sel), 0) * s.B : 0;
     const int chunks = (int)(((uint32_t)span + 31u) >> 5);
     const int c0 = (int)((int64_t)chunks * split / a.part.nsplit), c1 = (int)((int64_t)chunks * (split + 1) / a.part.nsplit);
 
@@ -89,46 +90,74 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     char *const mine = lds[wave];
 
     const int64_t base = (int64_t)b * s.sb + (int64_t)g * s.sh;
-    const uint8_t *const kc = (const uint8_t *)s.k + base + half * (D / 4), *const vc = (const uint8_t *)s.v + base + v_group * 16;
-    const uint8_t *const ksc = a.p.ks + (base >> 4) + half * (GROUPS / 2), *const vsc = a.p.vs + (base >> 4) + v_group;
+    const uint8_t *const kc = (const uint8_t *)s.k + base, *const vc = (const uint8_t *)s.v + base;
+    const uint8_t *const ksc = a.p.ks + (base >> 4), *const vsc = a.p.vs + (base >> 4);
     const int32_t *const list = a.sel_idx ? a.sel_idx + (int64_t)bg * a.n_sel : nullptr;
+    const uint32_t k_lane = (uint32_t)half * (D / 4), v_lane = (uint32_t)v_group * 16, ks_lane = (uint32_t)half * (GROUPS / 2), vs_lane = (uint32_t)v_group;
 
-    auto token_of = [&](int c) {   // of the lane's column of chunk c, or -1
-        const int p = 32 * c + col;
-        if (c >= c1 || p >= span) return -1;
-        int t = p;
-        if (list) {
-            const int slot = (int)a.div_B.div((uint32_t)p), e = list[slot];
-            t = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
+    typedef ChunkTokens<RUN> Tokens;
+    auto tokens_of = [&](int c) {   // of chunk c < c1 (behind it: of the last one once more)
+        Tokens x;
+        c = min(c, c1 - 1);
+        if constexpr (RUN) {
+            x.row = 32 * c;
+            if (list) {
+                const int slot = (int)a.div_B.div((uint32_t)(32 * c)), e = list[slot];
+                x.row = e >= 0 && e < nb ? e * s.B + (32 * c - slot * s.B) : -1;
+            }
+        } else {
+            const int p = 32 * c + col;
+            x.tok = -1;
+            if (p < span) {
+                x.tok = p;
+                if (list) {
+                    const int slot = (int)a.div_B.div((uint32_t)p), e = list[slot];
+                    x.tok = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
+                }
+            }
         }
-        return t < L ? t : -1;
+        return x;
     };
     struct Codes {
         uint4 k[GROUPS / 2], v[VLOADS];
         uint32_t ks, vs[VLOADS];
-        uint32_t live;
+        uint32_t live;       // bit t: token t of the chunk counts
     };
-    auto fetch = [&](int tok, Codes &x) {
-        x.live = (uint32_t)__ballot(tok >= 0);
+    // Tokens that are not there are read as another of the chunk, which is; a chunk of none as token 0, and is then left out.
+    auto fetch = [&](const Tokens &tk, Codes &x) __attribute__((always_inline)) {
+        if constexpr (RUN) {
+            const int n = tk.row < 0 ? 0 : min(max(L - tk.row, 0), 32);
+            x.live = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+            const int row = n > 0 ? tk.row : 0, last = n > 0 ? n - 1 : 0;
+            const int64_t at = (int64_t)row * s.st;
+            const uint8_t *const k0 = kc + at, *const v0 = vc + at, *const ks0 = ksc + (at >> 4), *const vs0 = vsc + (at >> 4);
+            const uint32_t st = (uint32_t)s.st;   // (32 rows lie within 2^31 bytes: launch_packed_attn)
+            const uint32_t ko = (uint32_t)min(col, last) * st;
 #pragma unroll
-        for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = make_uint4(0, 0, 0, 0);
-        x.ks = 0;
-        if (tok >= 0) {
+            for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = *(const uint4 *)(k0 + (ko + k_lane + 16 * i));
+            if constexpr (D == 128) x.ks = *(const uint16_t *)(ks0 + ((ko >> 4) + ks_lane));
+            else x.ks = ks0[(ko >> 4) + ks_lane];
+#pragma unroll
+            for (int i = 0; i < VLOADS; ++i) {
+                const uint32_t vo = (uint32_t)min(v_token(i), last) * st;
+                x.v[i] = *(const uint4 *)(v0 + (vo + v_lane));
+                x.vs[i] = vs0[(vo >> 4) + vs_lane];
+            }
+        } else {
+            const bool there = tk.tok >= 0 && tk.tok < L;
+            const unsigned long long who = __ballot(there);
+            x.live = (uint32_t)who;
+            const int tok = there ? tk.tok : (who ? __builtin_amdgcn_readlane(tk.tok, __builtin_ctzll(who)) : 0);
             const int64_t o = (int64_t)tok * s.st;
 #pragma unroll
-            for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = *(const uint4 *)(kc + o + 16 * i);
-            if constexpr (D == 128) x.ks = *(const uint16_t *)(ksc + (o >> 4));
-            else x.ks = ksc[o >> 4];
-        }
+            for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = *(const uint4 *)(kc + o + k_lane + 16 * i);
+            if constexpr (D == 128) x.ks = *(const uint16_t *)(ksc + (o >> 4) + ks_lane);
+            else x.ks = ksc[(o >> 4) + ks_lane];
 #pragma unroll
-        for (int i = 0; i < VLOADS; ++i) {
-            const int t = __shfl(tok, v_token(i));
-            x.v[i] = make_uint4(0, 0, 0, 0);
-            x.vs[i] = 0;
-            if (t >= 0) {
-                const int64_t o = (int64_t)t * s.st;
-                x.v[i] = *(const uint4 *)(vc + o);
-                x.vs[i] = vsc[o >> 4];
+            for (int i = 0; i < VLOADS; ++i) {
+                const int64_t vo = (int64_t)__shfl(tok, v_token(i)) * s.st;
+                x.v[i] = *(const uint4 *)(vc + vo + v_lane);
+                x.vs[i] = vsc[(vo >> 4) + vs_lane];
             }
         }
     };
@@ -138,7 +167,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     for (int j = 0; j < TILES; ++j)
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[j][i] = 0.f;
-    float m = -INFINITY, l = 0.f;   // m: of the column; l: of the lane's tokens
+    RowState st;
 
     // the lane's addresses for the transposing reads: token 4 half + (lane & 15) / 4 of eight, its 4 channels of tile j
     uint32_t v_at[2][TILES];
@@ -154,7 +183,8 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     }
     typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
 
-    auto work = [&](const Codes &x) {
+    auto work = [&](const Codes &x) __attribute__((always_inline)) {
+        if (x.live == 0) return;
         // V as bf16 into LDS
 #pragma unroll
         for (int i = 0; i < VLOADS; ++i) {
@@ -176,29 +206,15 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
 #pragma unroll
             for (int n = 0; n < N; ++n) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n][i], S, 0, 0, 0);
         }
-        if (x.live != 0xffffffffu) {
+        mask_scores(x.live, half, S);
+        follow_max(tile_max(S), a.scale_log2, st, O);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) S[i] = (x.live >> (8 * (i >> 2) + 4 * half + (i & 3))) & 1u ? S[i] : -INFINITY;
-        }
-        float top = S[0];
+        for (int i = 0; i < 16; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, st.neg_ref));
+        // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
+        float sum[4] = {S[0], S[1], S[2], S[3]};
 #pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, S[i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.scale_log2;
-        if (__any(top > m + kPackedSlack || (m == -INFINITY && top > -INFINITY))) {
-            const float m_new = fmaxf(m, top);
-            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
-            l *= alpha;
-#pragma unroll
-            for (int j = 0; j < TILES; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) O[j][i] *= alpha;
-            m = m_new;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, -ref));
-#pragma unroll
-        for (int i = 0; i < 16; ++i) l += S[i];
+        for (int i = 4; i < 16; ++i) sum[i & 3] += S[i];
+        st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             bf16x8 pf[N];
@@ -219,21 +235,27 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
         }
     };
 
-    {
+    if (c0 + wave < c1) {
+        Codes ring[RING];
         int c = c0 + wave;
-        Codes now, next;
-        fetch(token_of(c), now);
-        int tok = token_of(c + kPackedWaves);
-        while (c < c1) {
-            const int after = token_of(c + 2 * kPackedWaves);
-            fetch(tok, next);
-            tok = after;
-            work(now);
-            now = next;
-            c += kPackedWaves;
+#pragma unroll
+        for (int x = 0; x < RING - 1; ++x) fetch(tokens_of(c + x * kPackedWaves), ring[x]);
+        Tokens next = tokens_of(c + (RING - 1) * kPackedWaves);
+        for (;;) {
+            bool done = false;
+#pragma unroll
+            for (int x = 0; x < RING; ++x) {   // (in turn, so that no registers move)
+                const Tokens now = next;
+                next = tokens_of(c + RING * kPackedWaves);
+                fetch(now, ring[(x + RING - 1) % RING]);
+                work(ring[x]);
+                c += kPackedWaves;
+                if (c >= c1) { done = true; break; }
+            }
+            if (done) break;
         }
     }
-    l += __shfl_xor(l, 32);
+    float l = sum_xor32(st.l), m = l != 0.f ? -st.neg_ref : -INFINITY;   // (l may be NaN)
 
     // ---- the wavefronts' results into one: 2 and 3 into 0 and 1, then 1 into 0 ----
     constexpr int kParts = TILES * 16;   // values of a lane
@@ -295,11 +317,16 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st)
 {
     const Shape &s = p.s;
-    const int tiles = packed_row_tiles(s), pairs = s.batch * s.Hkv;
-    const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, pairs, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
+    const int tiles = packed_row_tiles(s);
+    const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
                            make_fastdiv((uint32_t)s.M), make_fastdiv((uint32_t)tiles), kLog2e / sqrtf((float)s.D)};
-    const dim3 grid(pairs, tiles * part.nsplit);
-#define SPECPV_ATTN(T, DD) hipLaunchKernelGGL((packed_attn_kernel<T, DD>), grid, dim3(64 * kPackedWaves), 0, st, a)
+    const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
+    const bool run = (!sel_idx || s.B % 32 == 0) && s.st < ((int64_t)1 << 26);
+#define SPECPV_ATTN(T, DD)                                                                                             \
+    do {                                                                                                               \
+        if (run) hipLaunchKernelGGL((packed_attn_kernel<T, DD, true>), grid, dim3(64 * kPackedWaves), 0, st, a);       \
+        else hipLaunchKernelGGL((packed_attn_kernel<T, DD, false>), grid, dim3(64 * kPackedWaves), 0, st, a);          \
+    } while (0)
     if (dtype == SPECPV_BF16) {
         if (s.D == 128) SPECPV_ATTN(bf16_t, 128); else SPECPV_ATTN(bf16_t, 64);
     } else {
