@@ -662,11 +662,11 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
     return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
 }
 
-// Splits: as many as have a place at once, two workgroups of four wavefronts a CU.
-static int64_t packed_splits(const Shape &s, int64_t n_blocks)
+// Splits: as many as have a place at once, two workgroups a CU.
+static int64_t packed_splits(const Shape &s, int dtype, int64_t n_blocks)
 {
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
-    const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s);
+    const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype);
     int64_t ns = 2 * (int64_t)device_cu_count() / columns;
     if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
     if (ns > 128) ns = 128;
@@ -951,10 +951,10 @@ size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tr
     if (!tree) return kArriveBytes + 256;
     if (check_tree(&plain, tree, false) != SPECPV_OK) return 0;
     const Shape s = make_shape(&plain, tree);
-    size_t need = packed_bytes(s, kv->dtype, packed_splits(s, s.max_blocks));
+    size_t need = packed_bytes(s, kv->dtype, packed_splits(s, kv->dtype, s.max_blocks));
     if (cfg) {
         const int64_t n_sel = (int64_t)cfg->n_sink_blocks + cfg->k_blocks + cfg->n_recent_blocks + cfg->n_extra_slots;
-        const size_t lists = packed_bytes(s, kv->dtype, packed_splits(s, n_sel)), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
+        const size_t lists = packed_bytes(s, kv->dtype, packed_splits(s, kv->dtype, n_sel)), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
         if (lists > need) need = lists;
         if (scores > need) need = scores;
     }
@@ -986,9 +986,9 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     const PackedShape p = make_packed(kv, tree);
     const Shape &s = p.s;
     if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, 1)) return SPECPV_EWORKSPACE;
-    int64_t ns = packed_splits(s, sel_idx ? n_sel : s.max_blocks);
+    int64_t ns = packed_splits(s, kv->dtype, sel_idx ? n_sel : s.max_blocks);
     while (ns > 1 && packed_bytes(s, kv->dtype, ns) > workspace_bytes) --ns;
-    if ((int64_t)packed_row_tiles(s) * ns > 65535) return SPECPV_ELIMIT;
+    if ((int64_t)packed_row_tiles(s, kv->dtype) * ns > 65535) return SPECPV_ELIMIT;
     const size_t rows = (size_t)s.batch * s.Hq * ns * s.M;
     char *const at = (char *)workspace + kArriveBytes;
     const Partials part{(float *)at, (float *)(at + align_up(rows * packed_row_bytes(s, kv->dtype))), (int)ns, packed_half(s, kv->dtype) ? 1 : 0, 0, nullptr};

@@ -64,8 +64,10 @@ hipError_t launch_packed_gather(const PackedShape &p, int dtype, const int32_t *
                                 void *out_k, void *out_v, int32_t *out_len, hipStream_t st);
 
 
-// Context part of the attention (packed_attn.hip): part.nsplit splits of row tiles of 32.
-static inline int packed_row_tiles(const Shape &s) { return (s.M * s.G + 31) / 32; }
+// Context part of the attention (packed_attn.hip): part.nsplit splits of row tiles of 16 or 32.
+// (fp32 at 128 channels has registers for 16 rows' three operands only)
+static inline int packed_row_tile(const Shape &s, int dtype) { return s.M * s.G <= 16 || (dtype == SPECPV_F32 && s.D == 128) ? 16 : 32; }
+static inline int packed_row_tiles(const Shape &s, int dtype) { return (s.M * s.G + packed_row_tile(s, dtype) - 1) / packed_row_tile(s, dtype); }
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st);
 
 }  // namespace specpv

@@ -23,7 +23,8 @@ struct PackedAttnArgs {
     float scale_log2;
 };
 
-constexpr int kPackedWaves = 4;
+// wavefronts of a workgroup, each with every so-manieth chunk of its split
+constexpr int packed_waves(int rt, bool f32) { return rt == 16 && !f32 ? 6 : 4; }
 
 // One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.
 template <typename T> struct Pieces { static constexpr int N = sizeof(T) == 2 ? 1 : 3; };
@@ -34,20 +35,60 @@ template <bool RUN> struct ChunkTokens;
 template <> struct ChunkTokens<true> { int row; };
 template <> struct ChunkTokens<false> { int tok; };
 
-template <typename T, int D, bool RUN>
-__global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(PackedAttnArgs a)
+template <bool STREAM, typename V> __device__ __forceinline__ V load_codes(const V *p)
 {
-    constexpr int N = Pieces<T>::N, STEPS = D / 16, GROUPS = D / 32, TILES = D / 32, VLOADS = D / 64;
-    constexpr int RING = N == 1 ? 3 : 2;              // chunks in registers: this one and those under way
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+
+// RT query rows a wavefront.  32: v_mfma_f32_32x32x16, two lanes a column; 16: v_mfma_f32_16x16x32, four lanes a column, half of the
+// registers and of the softmax, for few rows.  A column's lanes share the channels of the first product and the tokens of the second.
+template <int RT, int D> struct RowTile;
+template <int D> struct RowTile<32, D> {
+    typedef f32x16 Acc;
+    static constexpr int REGS = 16, KT = 1, VSTEPS = 2;
+    static __device__ __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ int token(int, int i, int part) { return 8 * (i >> 2) + 4 * part + (i & 3); }   // of score register i
+    static __device__ __forceinline__ float col_max(float x) { return max_xor32(x); }
+    static __device__ __forceinline__ float col_sum(float x) { return sum_xor32(x); }
+};
+template <int D> struct RowTile<16, D> {
+    typedef __attribute__((ext_vector_type(4))) float Acc;
+    static constexpr int REGS = 4, KT = 2, VSTEPS = 1;
+    static __device__ __forceinline__ Acc mfma(bf16x8 a, bf16x8 b, Acc c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ int token(int kt, int i, int part) { return 16 * kt + 4 * part + i; }
+    static __device__ __forceinline__ float xor16(float x, bool sum)
+    {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return sum ? __uint_as_float(r[0]) + __uint_as_float(r[1]) : fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    static __device__ __forceinline__ float col_max(float x) { return max_xor32(xor16(x, false)); }
+    static __device__ __forceinline__ float col_sum(float x) { return sum_xor32(xor16(x, true)); }
+};
+
+template <typename T, int D, int RT, bool RUN>
+__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && sizeof(T) == 2 ? 3 : 2) void packed_attn_kernel(PackedAttnArgs a)
+{
+    typedef RowTile<RT, D> Tile;
+    typedef typename Tile::Acc Acc;
+    constexpr int N = Pieces<T>::N, GROUPS = D / 32, KT = Tile::KT, REGS = Tile::REGS;
+    constexpr int PARTS = 64 / RT, SHARE = D / PARTS, STEPS = SHARE / 8;   // lanes of a column; their channels, and steps of the product
+    constexpr int KWORDS = SHARE / 8;                 // 4-byte words of K codes of a lane and tile
+    constexpr int OT = D / RT, VLOADS = D / 64;
+    constexpr int RING = N == 1 && RUN ? 3 : 2;              // chunks in registers: this one and those under way
+    constexpr int WAVES = packed_waves(RT, N > 1);
+    constexpr bool STREAM = RT == 16 && N == 1;       // codes past the caches: they are read once (one row tile)
     constexpr int VROW = D * 2;                       // bytes of a V row in LDS
-    __shared__ __align__(16) char lds[kPackedWaves][32 * VROW];
-    __shared__ float2 ml_lds[kPackedWaves][64];
+    constexpr int VALUES = OT * REGS;                 // results of a lane
+    constexpr int ROOM = 32 * VROW > VALUES * 256 ? 32 * VROW : VALUES * 256;
+    __shared__ __align__(16) char lds[WAVES][ROOM];   // V rows of each wavefront; at the end their results
+    __shared__ float2 ml_lds[WAVES][64];
     const Shape &s = a.p.s;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int col = lane & 31, half = lane >> 5;
+    const int col = lane & (RT - 1), part = lane / RT;
     const int bg = blockIdx.x, b = (int)a.div_hkv.div((uint32_t)bg), g = bg - b * s.Hkv;
     const int split = (int)a.div_tiles.div(blockIdx.y), tile = (int)blockIdx.y - split * a.row_tiles;
-    const int R = s.M * s.G, r = tile * 32 + col;
+    const int R = s.M * s.G, r = tile * RT + col;
     const bool row_live = r < R;
     const int64_t cap = (int64_t)s.max_blocks * s.B;
     const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
@@ -57,11 +98,11 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     const int chunks = (int)(((uint32_t)span + 31u) >> 5);
     const int c0 = (int)((int64_t)chunks * split / a.part.nsplit), c1 = (int)((int64_t)chunks * (split + 1) / a.part.nsplit);
 
-    // ---- query rows: the B operand of step i is channels 32 * (half * GROUPS / 2 + i / 4) + 8 * (i & 3) .. + 7 ----
+    // ---- query rows: the B operand of step i is channels part * SHARE + 8 i .. + 7 ----
     bf16x8 q[N][STEPS];
     {
         const int rr = min(r, R - 1), hh = (int)a.div_M.div((uint32_t)rr), j = rr - hh * s.M;
-        const T *row = (const T *)s.q + (((int64_t)b * s.M + j) * s.Hq + (int64_t)g * s.G + hh) * D + half * (D / 2);
+        const T *row = (const T *)s.q + (((int64_t)b * s.M + j) * s.Hq + (int64_t)g * s.G + hh) * D + part * SHARE;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             if constexpr (N == 1) {
@@ -80,10 +121,12 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     // ---- where this lane's V loads come from and go to ----
     // D = 128: lanes 4 u .. 4 u + 3 a token's four groups, 16 lanes tokens 0, 4, 8, 12 (+ lane / 16, + 16 x); D = 64: two
     // groups, 16 lanes 8 tokens in a row.  In LDS a row's 64-byte units and their 16-byte pieces are permuted by the token, so that
-    // the 16 lanes of a write cover all banks, and so do the four rows of 64 bytes that half a wavefront's transposing read takes.
+    // the 16 lanes of a write cover all banks, and so do the rows that half a wavefront's transposing read takes (RT = 32: four of
+    // 64 bytes, RT = 16: eight of 32).
     auto v_token = [&](int x) { return D == 128 ? 4 * ((lane >> 2) & 3) + (lane >> 4) + 16 * x : lane >> 1; };
     auto v_place = [&](int t, int unit, int piece) {   // byte of a 16-byte piece
-        return D == 128 ? t * VROW + ((unit ^ (t & 3)) << 6) + ((piece ^ ((t >> 2) & 3)) << 4)
+        const int u = t >> 2 & 3;
+        return D == 128 ? t * VROW + ((unit ^ (t & 3)) << 6) + ((piece ^ ((u & 1) << 1 | u >> 1)) << 4)
                         : t * VROW + ((unit ^ ((t >> 1) & 1)) << 6) + ((piece ^ ((t >> 1) & 3)) << 4);
     };
     const int v_group = lane & (GROUPS - 1);
@@ -93,7 +136,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
     const uint8_t *const kc = (const uint8_t *)s.k + base, *const vc = (const uint8_t *)s.v + base;
     const uint8_t *const ksc = a.p.ks + (base >> 4), *const vsc = a.p.vs + (base >> 4);
     const int32_t *const list = a.sel_idx ? a.sel_idx + (int64_t)bg * a.n_sel : nullptr;
-    const uint32_t k_lane = (uint32_t)half * (D / 4), v_lane = (uint32_t)v_group * 16, ks_lane = (uint32_t)half * (GROUPS / 2), vs_lane = (uint32_t)v_group;
+    const uint32_t k_lane = (uint32_t)part * (SHARE / 2), v_lane = (uint32_t)v_group * 16, ks_lane = (uint32_t)(part * SHARE) / 32, vs_lane = (uint32_t)v_group;
 
     typedef ChunkTokens<RUN> Tokens;
     auto tokens_of = [&](int c) {   // of chunk c < c1 (behind it: of the last one once more)
@@ -106,7 +149,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
                 x.row = e >= 0 && e < nb ? e * s.B + (32 * c - slot * s.B) : -1;
             }
         } else {
-            const int p = 32 * c + col;
+            const int p = 32 * c + (lane & 31);
             x.tok = -1;
             if (p < span) {
                 x.tok = p;
@@ -119,10 +162,24 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
         return x;
     };
     struct Codes {
-        uint4 k[GROUPS / 2], v[VLOADS];
-        uint32_t ks, vs[VLOADS];
+        uint32_t k[KT][KWORDS], ks[KT];
+        uint4 v[VLOADS];
+        uint32_t vs[VLOADS];
         uint32_t live;       // bit t: token t of the chunk counts
     };
+    auto k_words = [&](const uint8_t *p, uint32_t (&w)[KWORDS]) __attribute__((always_inline)) {
+        if constexpr (KWORDS == 2) {
+            const u32x2 u = load_codes<STREAM>((const u32x2 *)p);
+            w[0] = u[0]; w[1] = u[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < KWORDS; i += 4) {
+                const u32x4 u = load_codes<STREAM>((const u32x4 *)(p + 4 * i));
+                w[i] = u[0]; w[i + 1] = u[1]; w[i + 2] = u[2]; w[i + 3] = u[3];
+            }
+        }
+    };
+    auto k_scale = [&](const uint8_t *p) __attribute__((always_inline)) { return SHARE == 64 ? (uint32_t) * (const uint16_t *)p : (uint32_t)*p; };
     // Tokens that are not there are read as another of the chunk, which is; a chunk of none as token 0, and is then left out.
     auto fetch = [&](const Tokens &tk, Codes &x) __attribute__((always_inline)) {
         if constexpr (RUN) {
@@ -132,15 +189,16 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
             const int64_t at = (int64_t)row * s.st;
             const uint8_t *const k0 = kc + at, *const v0 = vc + at, *const ks0 = ksc + (at >> 4), *const vs0 = vsc + (at >> 4);
             const uint32_t st = (uint32_t)s.st;   // (32 rows lie within 2^31 bytes: launch_packed_attn)
-            const uint32_t ko = (uint32_t)min(col, last) * st;
 #pragma unroll
-            for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = *(const uint4 *)(k0 + (ko + k_lane + 16 * i));
-            if constexpr (D == 128) x.ks = *(const uint16_t *)(ks0 + ((ko >> 4) + ks_lane));
-            else x.ks = ks0[(ko >> 4) + ks_lane];
+            for (int kt = 0; kt < KT; ++kt) {
+                const uint32_t ko = (uint32_t)min(col + RT * kt, last) * st;
+                k_words(k0 + (ko + k_lane), x.k[kt]);
+                x.ks[kt] = k_scale(ks0 + ((ko >> 4) + ks_lane));
+            }
 #pragma unroll
             for (int i = 0; i < VLOADS; ++i) {
                 const uint32_t vo = (uint32_t)min(v_token(i), last) * st;
-                x.v[i] = *(const uint4 *)(v0 + (vo + v_lane));
+                x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(v0 + (vo + v_lane))));
                 x.vs[i] = vs0[(vo >> 4) + vs_lane];
             }
         } else {
@@ -148,37 +206,39 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
             const unsigned long long who = __ballot(there);
             x.live = (uint32_t)who;
             const int tok = there ? tk.tok : (who ? __builtin_amdgcn_readlane(tk.tok, __builtin_ctzll(who)) : 0);
-            const int64_t o = (int64_t)tok * s.st;
 #pragma unroll
-            for (int i = 0; i < GROUPS / 2; ++i) x.k[i] = *(const uint4 *)(kc + o + k_lane + 16 * i);
-            if constexpr (D == 128) x.ks = *(const uint16_t *)(ksc + (o >> 4) + ks_lane);
-            else x.ks = ksc[(o >> 4) + ks_lane];
+            for (int kt = 0; kt < KT; ++kt) {
+                const int64_t o = (int64_t)(KT == 1 ? tok : __shfl(tok, col + RT * kt)) * s.st;
+                k_words(kc + o + k_lane, x.k[kt]);
+                x.ks[kt] = k_scale(ksc + (o >> 4) + ks_lane);
+            }
 #pragma unroll
             for (int i = 0; i < VLOADS; ++i) {
                 const int64_t vo = (int64_t)__shfl(tok, v_token(i)) * s.st;
-                x.v[i] = *(const uint4 *)(vc + vo + v_lane);
+                x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(vc + vo + v_lane)));
                 x.vs[i] = vsc[(vo >> 4) + vs_lane];
             }
         }
     };
 
-    f32x16 O[TILES];
+    Acc O[OT];
 #pragma unroll
-    for (int j = 0; j < TILES; ++j)
+    for (int j = 0; j < OT; ++j)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) O[j][i] = 0.f;
-    RowState st;
+        for (int i = 0; i < REGS; ++i) O[j][i] = 0.f;
+    float neg_ref = 3e38f, sum_l = 0.f;   // (see RowState)
 
-    // the lane's addresses for the transposing reads: token 4 half + (lane & 15) / 4 of eight, its 4 channels of tile j
-    uint32_t v_at[2][TILES];
+    // the lane's addresses for the transposing reads: its token of the four that 16 lanes turn, its 4 channels of tile j
+    uint32_t v_at[2][OT];
     {
-        const int sl = lane & 15, grp = (lane >> 4) & 1;
+        const int sl = lane & 15;
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
-            for (int j = 0; j < TILES; ++j) {
-                const int t = 8 * hf + 4 * half + (sl >> 2), byte = 32 * grp + 8 * (sl & 3);
-                v_at[hf][j] = (uint32_t)(v_place(t, j, byte >> 4) + (byte & 15));
+            for (int j = 0; j < OT; ++j) {
+                const int t = (RT == 32 ? 8 : 16) * hf + 4 * part + (sl >> 2);
+                const int byte = 2 * RT * j + (RT == 32 ? 32 * ((lane >> 4) & 1) : 0) + 8 * (sl & 3);   // of the row
+                v_at[hf][j] = (uint32_t)(v_place(t, byte >> 6, (byte >> 4) & 3) + (byte & 15));
             }
     }
     typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
@@ -194,43 +254,66 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
 #pragma unroll
             for (int e = 0; e < 4; ++e) *(uint4 *)(mine + v_place(t, v_group, e)) = decode8_bf16(w[e], sc);
         }
-        f32x16 S;
+        Acc S[KT];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+        for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            const uint4 c4 = x.k[i >> 2];
-            const uint32_t w = (i & 3) == 0 ? c4.x : ((i & 3) == 1 ? c4.y : ((i & 3) == 2 ? c4.z : c4.w));
-            const float sc = scale_of((i >> 2) ? x.ks >> 8 : x.ks & 0xffu);
-            const bf16x8 kf = __builtin_bit_cast(bf16x8, decode8_bf16(w, sc));
+            for (int i = 0; i < REGS; ++i) S[kt][i] = 0.f;
 #pragma unroll
-            for (int n = 0; n < N; ++n) S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[n][i], S, 0, 0, 0);
+            for (int i = 0; i < STEPS; ++i) {
+                const float sc = scale_of(SHARE == 64 ? (i >> 2 ? x.ks[kt] >> 8 : x.ks[kt] & 0xffu) : x.ks[kt]);
+                const bf16x8 kf = __builtin_bit_cast(bf16x8, decode8_bf16(x.k[kt][i], sc));
+#pragma unroll
+                for (int n = 0; n < N; ++n) S[kt] = Tile::mfma(kf, q[n][i], S[kt]);
+            }
         }
-        mask_scores(x.live, half, S);
-        follow_max(tile_max(S), a.scale_log2, st, O);
+        if (x.live != 0xffffffffu) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, st.neg_ref));
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < REGS; ++i) S[kt][i] = x.live >> Tile::token(kt, i, part) & 1u ? S[kt][i] : -INFINITY;
+        }
+        // the reference maximum moves where a lane's own maximum runs more than 2^8 ahead of it
+        float top = S[0][0];
+#pragma unroll
+        for (int i = 1; i < KT * REGS; ++i) top = fmaxf(top, S[i / REGS][i % REGS]);
+        if (__any(fmaf(top, a.scale_log2, neg_ref) > kRescaleSlack)) {
+            const float z = Tile::col_max(top) * a.scale_log2, ref = -neg_ref, ref_new = z > ref + kRescaleSlack ? z : ref;
+            const float alpha = __builtin_amdgcn_exp2f(ref - ref_new);
+            const bool rescale = __any(alpha != 1.f && sum_l != 0.f);
+            neg_ref = -ref_new;
+            sum_l *= alpha;
+            if (rescale) {
+#pragma unroll
+                for (int j = 0; j < OT; ++j)
+#pragma unroll
+                    for (int i = 0; i < REGS; ++i) O[j][i] *= alpha;
+            }
+        }
+        float w[KT * REGS];
+#pragma unroll
+        for (int i = 0; i < KT * REGS; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(S[i / REGS][i % REGS], a.scale_log2, neg_ref));
         // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
-        float sum[4] = {S[0], S[1], S[2], S[3]};
+        float sum[4] = {w[0], w[1], w[2], w[3]};
 #pragma unroll
-        for (int i = 4; i < 16; ++i) sum[i & 3] += S[i];
-        st.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        for (int i = 4; i < KT * REGS; ++i) sum[i & 3] += w[i];
+        sum_l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < Tile::VSTEPS; ++ks) {
             bf16x8 pf[N];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float f = S[8 * ks + e];
+                float f = w[8 * ks + e];
 #pragma unroll
                 for (int n = 0; n < N; ++n) { pf[n][e] = (__bf16)f; f -= (float)pf[n][e]; }
             }
 #pragma unroll
-            for (int j = 0; j < TILES; ++j) {
+            for (int j = 0; j < OT; ++j) {
                 const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[0][j] + ks * 16 * VROW));
                 const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[1][j] + ks * 16 * VROW));
-                const auto both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                for (int n = 0; n < N; ++n) O[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), pf[n], O[j], 0, 0, 0);
+                for (int n = 0; n < N; ++n) O[j] = Tile::mfma(vf, pf[n], O[j]);
             }
         }
     };
@@ -239,100 +322,96 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_attn_kernel(Packe
         Codes ring[RING];
         int c = c0 + wave;
 #pragma unroll
-        for (int x = 0; x < RING - 1; ++x) fetch(tokens_of(c + x * kPackedWaves), ring[x]);
-        Tokens next = tokens_of(c + (RING - 1) * kPackedWaves);
+        for (int x = 0; x < RING - 1; ++x) fetch(tokens_of(c + x * WAVES), ring[x]);
+        Tokens next = tokens_of(c + (RING - 1) * WAVES);
         for (;;) {
             bool done = false;
 #pragma unroll
             for (int x = 0; x < RING; ++x) {   // (in turn, so that no registers move)
                 const Tokens now = next;
-                next = tokens_of(c + RING * kPackedWaves);
+                next = tokens_of(c + RING * WAVES);
                 fetch(now, ring[(x + RING - 1) % RING]);
                 work(ring[x]);
-                c += kPackedWaves;
+                c += WAVES;
                 if (c >= c1) { done = true; break; }
             }
             if (done) break;
         }
     }
-    float l = sum_xor32(st.l), m = l != 0.f ? -st.neg_ref : -INFINITY;   // (l may be NaN)
-
-    // ---- the wavefronts' results into one: 2 and 3 into 0 and 1, then 1 into 0 ----
-    constexpr int kParts = TILES * 16;   // values of a lane
-    float *const room = (float *)lds;    // [2][kParts][64]
-    static_assert(2 * kParts * 64 * 4 <= (int)sizeof(lds), "room for two wavefronts' results");
+    // ---- the wavefronts' results into one: all of them to LDS, and each wavefront merges and stores every so-manieth four channels ----
+    float l = Tile::col_sum(sum_l), m = l != 0.f ? -neg_ref : -INFINITY;   // (l may be NaN)
+    ml_lds[wave][lane] = make_float2(m, l);
+    float4 *const own = (float4 *)lds[wave];     // [VALUES / 4][64]
 #pragma unroll
-    for (int n = kPackedWaves / 2; n > 0; n >>= 1) {
-        __syncthreads();
-        if (wave >= n && wave < 2 * n) {
-            ml_lds[wave - n][lane] = make_float2(m, l);
-#pragma unroll
-            for (int j = 0; j < TILES; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) room[((wave - n) * kParts + j * 16 + i) * 64 + lane] = O[j][i];
-        }
-        __syncthreads();
-        if (wave < n) {
-            const float2 o = ml_lds[wave][lane];
-            const float m_new = fmaxf(m, o.x), ref = m_new == -INFINITY ? 0.f : m_new;
-            const float w0 = __builtin_amdgcn_exp2f(m - ref), w1 = __builtin_amdgcn_exp2f(o.x - ref);
-            l = l * w0 + o.y * w1;
-            m = m_new;
-#pragma unroll
-            for (int j = 0; j < TILES; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) O[j][i] = O[j][i] * w0 + room[(wave * kParts + j * 16 + i) * 64 + lane] * w1;
-        }
+    for (int i = 0; i < VALUES / 4; ++i) {
+        const Acc &o = O[4 * i / REGS];
+        own[i * 64 + lane] = make_float4(o[4 * i % REGS], o[4 * i % REGS + 1], o[4 * i % REGS + 2], o[4 * i % REGS + 3]);
     }
-    if (wave || !row_live) return;
+    __syncthreads();
+    float wt[WAVES];
+    m = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) m = fmaxf(m, ml_lds[x][lane].x);
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int x = 0; x < WAVES; ++x) {
+        const float2 o = ml_lds[x][lane];
+        wt[x] = __builtin_amdgcn_exp2f(o.x - ref);
+        l = fmaf(o.y, wt[x], l);
+    }
+    if (!row_live) return;
     const int64_t prow = ((int64_t)bg * a.part.nsplit + split) * R + r;
     // (the combine kernel takes a partial by l > 0: a sum that is no number is handed on in the maximum's place)
-    if (half == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
-    if (a.part.o_half) {
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-        typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-        _Float16 *out = (_Float16 *)a.part.o + prow * D;
+    if (wave == 0 && part == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-        for (int j = 0; j < TILES; ++j)
+    for (int i = 0; i < (VALUES / 4 + WAVES - 1) / WAVES; ++i) {
+        const int at = i * WAVES + wave;
+        if (at >= VALUES / 4) break;
+        float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                f16x4 v;
+        for (int x = 0; x < WAVES; ++x) {
+            const float4 v = ((const float4 *)lds[x])[at * 64 + lane];
+            o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
+        }
+        const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
+        if (a.part.o_half) {
+            typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+            f16x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float o = O[j][i + e] * inv;
-                    v[e] = (_Float16)(o > 65504.f ? 65504.f : (o < -65504.f ? -65504.f : o));   // (NaN stays)
-                }
-                *(f16x4 *)(out + 32 * j + 8 * (i >> 2) + 4 * half) = v;
+            for (int e = 0; e < 4; ++e) {
+                const float y = o[e] * inv;
+                v[e] = (_Float16)(y > 65504.f ? 65504.f : (y < -65504.f ? -65504.f : y));   // (NaN stays)
             }
-    } else {
-        float *out = a.part.o + prow * D;
-#pragma unroll
-        for (int j = 0; j < TILES; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *(float4 *)(out + partial_pos(32 * j + 8 * (i >> 2) + 4 * half, D)) = make_float4(O[j][i], O[j][i + 1], O[j][i + 2], O[j][i + 3]);
+            *(f16x4 *)((_Float16 *)a.part.o + prow * D + ch) = v;
+        } else {
+            *(float4 *)(a.part.o + prow * D + partial_pos(ch, D)) = make_float4(o[0], o[1], o[2], o[3]);
+        }
     }
 }
 
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st)
 {
     const Shape &s = p.s;
-    const int tiles = packed_row_tiles(s);
+    const int rt = packed_row_tile(s, dtype), tiles = packed_row_tiles(s, dtype);
     const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
                            make_fastdiv((uint32_t)s.M), make_fastdiv((uint32_t)tiles), kLog2e / sqrtf((float)s.D)};
     const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
     const bool run = (!sel_idx || s.B % 32 == 0) && s.st < ((int64_t)1 << 26);
-#define SPECPV_ATTN(T, DD)                                                                                             \
-    do {                                                                                                               \
-        if (run) hipLaunchKernelGGL((packed_attn_kernel<T, DD, true>), grid, dim3(64 * kPackedWaves), 0, st, a);       \
-        else hipLaunchKernelGGL((packed_attn_kernel<T, DD, false>), grid, dim3(64 * kPackedWaves), 0, st, a);          \
+#define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
+    do {                                                                                                                                \
+        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4)), 0, st, a);                \
+        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4)), 0, st, a); \
     } while (0)
+#define SPECPV_ATTN(T, DD) do { if (run) SPECPV_ATTN_R(T, DD, true); else SPECPV_ATTN_R(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {
         if (s.D == 128) SPECPV_ATTN(bf16_t, 128); else SPECPV_ATTN(bf16_t, 64);
     } else {
         if (s.D == 128) SPECPV_ATTN(float, 128); else SPECPV_ATTN(float, 64);
     }
 #undef SPECPV_ATTN
+#undef SPECPV_ATTN_R
     return hipGetLastError();
 }
 
