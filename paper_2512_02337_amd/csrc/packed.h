@@ -65,6 +65,8 @@ hipError_t launch_packed_gather(const PackedShape &p, int dtype, const int32_t *
 
 
 // Context part of the attention (packed_attn.hip): part.nsplit splits of row tiles of 16 or 32.
+// Whether a chunk's 32 tokens follow each other: the whole cache, or blocks of whole chunks (rows no more than 2^26 bytes apart).
+static inline bool packed_runs(const Shape &s, bool lists) { return (!lists || s.B % 32 == 0) && s.st < ((int64_t)1 << 26); }
 // (fp32 at 128 channels has registers for 16 rows' three operands only)
 static inline int packed_row_tile(const Shape &s, int dtype) { return s.M * s.G <= 16 || (dtype == SPECPV_F32 && s.D == 128) ? 16 : 32; }
 static inline int packed_row_tiles(const Shape &s, int dtype) { return (s.M * s.G + packed_row_tile(s, dtype) - 1) / packed_row_tile(s, dtype); }

@@ -35,6 +35,23 @@ template <bool RUN> struct ChunkTokens;
 template <> struct ChunkTokens<true> { int row; };
 template <> struct ChunkTokens<false> { int tok; };
 
+// Four adjacent channels of a partial's row (see Partials): sums, and the factor that normalises them.
+__device__ __forceinline__ void store_partial(const Partials &part, int64_t row, int ch, int D, const float (&o)[4], float inv)
+{
+    if (part.o_half) {
+        typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+        f16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float y = o[e] * inv;
+            v[e] = (_Float16)(y > 65504.f ? 65504.f : (y < -65504.f ? -65504.f : y));   // (NaN stays)
+        }
+        *(f16x4 *)((_Float16 *)part.o + row * D + ch) = v;
+    } else {
+        *(float4 *)(part.o + row * D + partial_pos(ch, D)) = make_float4(o[0], o[1], o[2], o[3]);
+    }
+}
+
 template <bool STREAM, typename V> __device__ __forceinline__ V load_codes(const V *p)
 {
     if constexpr (STREAM) return __builtin_nontemporal_load(p);
@@ -226,7 +243,7 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && 
     for (int j = 0; j < OT; ++j)
 #pragma unroll
         for (int i = 0; i < REGS; ++i) O[j][i] = 0.f;
-    float neg_ref = 3e38f, sum_l = 0.f;   // (see RowState)
+    float neg_ref = 3e38f, sum_l = 0.f;   // minus the reference maximum, in log2 units; the lane's sum
 
     // the lane's addresses for the transposing reads: its token of the four that 16 lanes turn, its 4 channels of tile j
     uint32_t v_at[2][OT];
@@ -273,31 +290,34 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && 
 #pragma unroll
                 for (int i = 0; i < REGS; ++i) S[kt][i] = x.live >> Tile::token(kt, i, part) & 1u ? S[kt][i] : -INFINITY;
         }
-        // the reference maximum moves where a lane's own maximum runs more than 2^8 ahead of it
-        float top = S[0][0];
+        // The reference maximum moves where the weights say that it has been left behind: one above 2^12 makes its lane's sum larger
+        // than that (so does the first chunk's, by a reference of -3e38, and one that is no number).  No maximum is looked for elsewhere.
+        float w[KT * REGS], sum;
+        auto weigh = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 1; i < KT * REGS; ++i) top = fmaxf(top, S[i / REGS][i % REGS]);
-        if (__any(fmaf(top, a.scale_log2, neg_ref) > kRescaleSlack)) {
-            const float z = Tile::col_max(top) * a.scale_log2, ref = -neg_ref, ref_new = z > ref + kRescaleSlack ? z : ref;
+            for (int i = 0; i < KT * REGS; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(S[i / REGS][i % REGS], a.scale_log2, neg_ref));
+            // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
+            float t[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+            for (int i = 4; i < KT * REGS; ++i) t[i & 3] += w[i];
+            sum = (t[0] + t[1]) + (t[2] + t[3]);
+        };
+        weigh();
+        if (__any(!(sum <= 4096.f))) {
+            float top = S[0][0];
+#pragma unroll
+            for (int i = 1; i < KT * REGS; ++i) top = fmaxf(top, S[i / REGS][i % REGS]);
+            const float z = Tile::col_max(top) * a.scale_log2, ref = -neg_ref, ref_new = z > ref ? z : ref;
             const float alpha = __builtin_amdgcn_exp2f(ref - ref_new);
-            const bool rescale = __any(alpha != 1.f && sum_l != 0.f);
             neg_ref = -ref_new;
             sum_l *= alpha;
-            if (rescale) {
 #pragma unroll
-                for (int j = 0; j < OT; ++j)
+            for (int j = 0; j < OT; ++j)
 #pragma unroll
-                    for (int i = 0; i < REGS; ++i) O[j][i] *= alpha;
-            }
+                for (int i = 0; i < REGS; ++i) O[j][i] *= alpha;
+            weigh();
         }
-        float w[KT * REGS];
-#pragma unroll
-        for (int i = 0; i < KT * REGS; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(S[i / REGS][i % REGS], a.scale_log2, neg_ref));
-        // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
-        float sum[4] = {w[0], w[1], w[2], w[3]};
-#pragma unroll
-        for (int i = 4; i < KT * REGS; ++i) sum[i & 3] += w[i];
-        sum_l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        sum_l += sum;
 #pragma unroll
         for (int ks = 0; ks < Tile::VSTEPS; ++ks) {
             bf16x8 pf[N];
@@ -376,29 +396,18 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && 
             o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
         }
         const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
-        if (a.part.o_half) {
-            typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
-            f16x4 v;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y = o[e] * inv;
-                v[e] = (_Float16)(y > 65504.f ? 65504.f : (y < -65504.f ? -65504.f : y));   // (NaN stays)
-            }
-            *(f16x4 *)((_Float16 *)a.part.o + prow * D + ch) = v;
-        } else {
-            *(float4 *)(a.part.o + prow * D + partial_pos(ch, D)) = make_float4(o[0], o[1], o[2], o[3]);
-        }
+        store_partial(a.part, prow, ch, D, o, inv);
     }
 }
 
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st)
 {
     const Shape &s = p.s;
+    const bool run = packed_runs(s, sel_idx != nullptr);
     const int rt = packed_row_tile(s, dtype), tiles = packed_row_tiles(s, dtype);
     const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
                            make_fastdiv((uint32_t)s.M), make_fastdiv((uint32_t)tiles), kLog2e / sqrtf((float)s.D)};
     const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
-    const bool run = (!sel_idx || s.B % 32 == 0) && s.st < ((int64_t)1 << 26);
 #define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
     do {                                                                                                                                \
         if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4)), 0, st, a);                \
