@@ -662,13 +662,14 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
     return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
 }
 
-// Splits: as many as have a place at once, two workgroups a CU.
+// Splits: as many as have a place at once.
 static int64_t packed_splits(const Shape &s, int dtype, int64_t n_blocks)
 {
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
     const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype);
-    int64_t ns = 2 * (int64_t)device_cu_count() / columns;
-    if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
+    const int64_t waves = packed_waves(packed_row_tile(s, dtype), dtype == SPECPV_F32, s.D);
+    int64_t ns = packed_places(s, dtype) * (int64_t)device_cu_count() / columns;
+    if (ns > (chunks + waves - 1) / waves) ns = (chunks + waves - 1) / waves;
     if (ns > 128) ns = 128;
     return ns < 1 ? 1 : ns;
 }

@@ -70,6 +70,15 @@ static inline bool packed_runs(const Shape &s, bool lists) { return (!lists || s
 // (fp32 at 128 channels has registers for 16 rows' three operands only)
 static inline int packed_row_tile(const Shape &s, int dtype) { return s.M * s.G <= 16 || (dtype == SPECPV_F32 && s.D == 128) ? 16 : 32; }
 static inline int packed_row_tiles(const Shape &s, int dtype) { return (s.M * s.G + packed_row_tile(s, dtype) - 1) / packed_row_tile(s, dtype); }
+// Wavefronts of a workgroup, each with every so-manieth chunk of its split; and workgroups that a CU has room for.  Tiles of 16 rows: three
+// wavefronts a SIMD, all in one workgroup, so that a split more does not mean a partial more.  (Six of them: a SIMD gets two of one workgroup and
+// none of the next, and half of the workgroups wait: one token over 128K, 31.3 us where this takes 27.0.)
+__host__ __device__ constexpr int packed_waves(int rt, bool f32, int D) { return rt == 16 && !f32 ? (D == 64 ? 16 : 12) : 4; }
+static inline int packed_places(const Shape &s, int dtype)
+{
+    if (dtype == SPECPV_F32) return s.D == 64 && s.M * s.G <= 16 ? 3 : 2;
+    return packed_row_tile(s, dtype) == 16 ? 1 : (s.D == 64 ? 3 : 2);
+}
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st);
 
 }  // namespace specpv

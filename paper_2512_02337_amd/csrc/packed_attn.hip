@@ -23,8 +23,6 @@ struct PackedAttnArgs {
     float scale_log2;
 };
 
-// wavefronts of a workgroup, each with every so-manieth chunk of its split
-constexpr int packed_waves(int rt, bool f32) { return rt == 16 && !f32 ? 6 : 4; }
 
 // One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.
 template <typename T> struct Pieces { static constexpr int N = sizeof(T) == 2 ? 1 : 3; };
@@ -84,7 +82,7 @@ template <int D> struct RowTile<16, D> {
 };
 
 template <typename T, int D, int RT, bool RUN>
-__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && sizeof(T) == 2 ? 3 : 2) void packed_attn_kernel(PackedAttnArgs a)
+__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4, D), RT == 16 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2) void packed_attn_kernel(PackedAttnArgs a)
 {
     typedef RowTile<RT, D> Tile;
     typedef typename Tile::Acc Acc;
@@ -93,7 +91,7 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), RT == 16 && 
     constexpr int KWORDS = SHARE / 8;                 // 4-byte words of K codes of a lane and tile
     constexpr int OT = D / RT, VLOADS = D / 64;
     constexpr int RING = N == 1 && RUN ? 3 : 2;              // chunks in registers: this one and those under way
-    constexpr int WAVES = packed_waves(RT, N > 1);
+    constexpr int WAVES = packed_waves(RT, N > 1, D);
     constexpr bool STREAM = RT == 16 && N == 1;       // codes past the caches: they are read once (one row tile)
     constexpr int VROW = D * 2;                       // bytes of a V row in LDS
     constexpr int VALUES = OT * REGS;                 // results of a lane
@@ -410,8 +408,8 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
 #define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
     do {                                                                                                                                \
-        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4)), 0, st, a);                \
-        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4)), 0, st, a); \
+        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4, DD)), 0, st, a);                \
+        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4, DD)), 0, st, a); \
     } while (0)
 #define SPECPV_ATTN(T, DD) do { if (run) SPECPV_ATTN_R(T, DD, true); else SPECPV_ATTN_R(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {

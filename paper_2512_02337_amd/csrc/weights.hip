@@ -59,7 +59,7 @@ __device__ __forceinline__ float fold32(const float (&v)[16], int lane)
 constexpr int kWeighWaves = 4;
 template <typename T, int D> struct WeighTile {
     static constexpr int E = Elem<T>::kPerVec, STEPS = D / (2 * E);        // channels of a lane's 16 bytes; products of a tile
-    static constexpr int TILES = STEPS * 2 * 4 <= 64 ? 2 : 1;              // tiles of 32 tokens of a wavefront: 64 registers of K
+    static constexpr int TILES = 1;              // tiles of 32 tokens of a wavefront: 64 registers of K
     static constexpr int PIECES = D / E;                                   // 16-byte pieces of a row
     static constexpr int ROWS = 32768 / (PIECES * 16);                     // query rows in LDS at a time
     // so that the 16 lanes that LDS serves at a time find their pieces in different banks
