@@ -5,8 +5,7 @@
 // a wavefront keeps its tokens' K rows in registers as the matrix instruction's A operand (rows = tokens), the query rows go
 // by as B (columns), 32 at a time out of LDS, and a lane adds up its column's weights for 16 tokens a tile.  The 32 columns
 // are folded once, at the end.  K is read once and nothing else of size is read or written.
-#include "internal.h"
-#include <type_traits>
+#include "summarize.h"
 
 namespace specpv {
 
@@ -56,12 +55,16 @@ __device__ __forceinline__ float fold32(const float (&v)[16], int lane)
     return d + __shfl_xor(d, 16);
 }
 
-constexpr int kWeighWaves = 4;
-template <typename T, int D> struct WeighTile {
+// WAVES: 4, or as many as a CU takes (MANY).  A stage's query rows are found and fetched by all of a workgroup's threads, on their way
+// to registers while the stage before is worked on; many rows are cheaper for many wavefronts at once, but one workgroup to a CU
+// has nobody to compute while it reads its K rows (launch_weigh).
+template <typename T, int D, bool MANY> struct WeighTile {
     static constexpr int E = Elem<T>::kPerVec, STEPS = D / (2 * E);        // channels of a lane's 16 bytes; products of a tile
-    static constexpr int TILES = 1;              // tiles of 32 tokens of a wavefront: 64 registers of K
     static constexpr int PIECES = D / E;                                   // 16-byte pieces of a row
-    static constexpr int ROWS = 32768 / (PIECES * 16);                     // query rows in LDS at a time
+    static constexpr int WAVES = !MANY ? 4 : (STEPS * 4 > 32 ? 8 : 16);    // (K rows: 32 registers, or 64)
+    static constexpr int MINE = PIECES == 32 ? 4 : 2;                      // pieces of a stage that a thread brings
+    static constexpr int ROWS = MINE * 64 * WAVES / PIECES;                // query rows of a stage
+    static_assert(ROWS % 32 == 0, "whole tiles");
     // so that the 16 lanes that LDS serves at a time find their pieces in different banks
     static __device__ __forceinline__ int place(int row, int piece)
     {
@@ -69,13 +72,13 @@ template <typename T, int D> struct WeighTile {
     }
 };
 
-template <typename T, int D, bool LISTS>
-__global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighKernelArgs k)
+template <typename T, int D, bool MANY, bool LISTS>
+__global__ __launch_bounds__((64 * WeighTile<T, D, MANY>::WAVES)) void weigh_kernel(WeighKernelArgs k)
 {
-    typedef WeighTile<T, D> W;
-    constexpr int E = W::E, STEPS = W::STEPS, TILES = W::TILES;
-    __shared__ uint4 q_lds[W::ROWS * W::PIECES];
-    __shared__ float lse_lds[W::ROWS];   // -lse * log2 e; -inf: no such row
+    typedef WeighTile<T, D, MANY> W;
+    constexpr int STEPS = W::STEPS, THREADS = 64 * W::WAVES;
+    __shared__ uint4 q_lds[2][W::ROWS * W::PIECES];
+    __shared__ float lse_lds[2][W::ROWS];   // -lse * log2 e; -inf: no such row
     const Shape &s = k.s;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.y, b = blockIdx.z, half = lane >> 5, col = lane & 31;
@@ -83,99 +86,89 @@ __global__ __launch_bounds__(64 * kWeighWaves, 2) void weigh_kernel(WeighKernelA
     const int64_t cap = (int64_t)s.max_blocks * s.B;
     const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
     const int nb = (int)k.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
-    int cnt = 0, span = L;   // entries of the list; positions that there are
-    if (LISTS) {
-        cnt = min(k.a.sel_count[bg], k.a.n_sel);
-        span = max(cnt, 0) * s.B;
-    }
-    const int p0 = (int)blockIdx.x * (kWeighWaves * 32 * TILES);
-    if (p0 >= span) return;
+    int span = L;   // positions that there are
+    if (LISTS) span = max(min(k.a.sel_count[bg], k.a.n_sel), 0) * s.B;
+    const int p0 = (int)blockIdx.x * (W::WAVES * 32);
+    if (p0 >= span || L == 0) return;
     // ---- the wavefront's K rows ----
-    int tok[TILES];
-    uint4 kk[TILES][STEPS];
-    const char *const k0 = (const char *)s.k + ((int64_t)b * s.sb + (int64_t)g * s.sh) * (int64_t)sizeof(T) + 16 * half;
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-        const int p = p0 + (wave * TILES + x) * 32 + col;
-        tok[x] = -1;
+    int tok = -1;
+    uint4 kk[STEPS];
+    {
+        const int p = p0 + wave * 32 + col;
         if (p < span) {
-            tok[x] = p;
+            tok = p;
             if (LISTS) {
                 const int slot = (int)k.div_B.div((uint32_t)p), e = k.a.sel_idx[bg * k.a.n_sel + slot];
-                tok[x] = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
+                tok = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
             }
-            if (tok[x] >= L) tok[x] = -1;
+            if (tok >= L) tok = -1;
         }
-        if (tok[x] >= 0) {
-            const char *row = k0 + (int64_t)tok[x] * s.st * (int64_t)sizeof(T);
+        const char *row = (const char *)s.k + ((int64_t)b * s.sb + (int64_t)g * s.sh + (int64_t)max(tok, 0) * s.st) * (int64_t)sizeof(T) + 16 * half;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) kk[x][i] = *(const uint4 *)(row + 32 * i);
-        } else {
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) kk[x][i] = make_uint4(0, 0, 0, 0);
-        }
+        for (int i = 0; i < STEPS; ++i) kk[i] = *(const uint4 *)(row + 32 * i);   // (a token that is not there: the first one, for nothing)
     }
-    float sum[TILES][16];
-#pragma unroll
-    for (int x = 0; x < TILES; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[x][i] = 0.f;
+    // ---- query rows r0 .. r0 + ROWS - 1: this thread's pieces, and the sums of the rows whose first pieces they are ----
     const int nodes = k.a.nodes ? min(k.a.n_nodes[b], k.a.max_nodes) : s.M;
     const int R = max(nodes, 0) * s.G;
-    for (int r0 = 0; r0 < R; r0 += W::ROWS) {
-        const int rows = min(W::ROWS, R - r0), padded = (rows + 31) & ~31;
-        if (r0) __syncthreads();
-        for (int at = threadIdx.x; at < padded * W::PIECES; at += 64 * kWeighWaves) {
-            const int row = at / W::PIECES, piece = at % W::PIECES;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            float neg = -INFINITY;
-            if (row < rows) {
-                const int i = (int)k.div_G.div((uint32_t)(r0 + row)), hh = r0 + row - i * s.G;
+    uint4 qp[W::MINE];
+    float neg[W::MINE];
+    auto fetch = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < W::MINE; ++x) {
+            const int at = (int)threadIdx.x + x * THREADS, row = r0 + at / W::PIECES, piece = at % W::PIECES;
+            qp[x] = make_uint4(0, 0, 0, 0);
+            neg[x] = -INFINITY;
+            if (row < R) {
+                const int i = (int)k.div_G.div((uint32_t)row), hh = row - i * s.G;
                 const int node = k.a.nodes ? k.a.nodes[(int64_t)b * k.a.max_nodes + i] : i;
                 if (node >= 0 && node < s.M) {
                     const int64_t qr = ((int64_t)b * s.M + node) * s.Hq + (int64_t)g * s.G + hh;
-                    v = ((const uint4 *)s.q)[qr * W::PIECES + piece];
+                    qp[x] = ((const uint4 *)s.q)[qr * W::PIECES + piece];
                     if (piece == 0) {
                         const float l = k.a.lse[qr];
-                        neg = l == -INFINITY ? -INFINITY : l * -kLog2e;   // (a row that attended nothing gives nothing)
+                        neg[x] = l == -INFINITY ? -INFINITY : l * -kLog2e;   // (a row that attended nothing gives nothing)
                     }
                 }
             }
-            q_lds[W::place(row, piece)] = v;
-            if (piece == 0) lse_lds[row] = neg;
         }
-        __syncthreads();
-        for (int t0 = 0; t0 < padded; t0 += 32) {
-            f32x16 sc[TILES];
+    };
+    float sum[16];
 #pragma unroll
-            for (int x = 0; x < TILES; ++x)
+    for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+    fetch(0);
+    for (int r0 = 0, buf = 0; r0 < R; r0 += W::ROWS, buf ^= 1) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sc[x][i] = 0.f;
+        for (int x = 0; x < W::MINE; ++x) {
+            const int at = (int)threadIdx.x + x * THREADS, row = at / W::PIECES, piece = at % W::PIECES;
+            q_lds[buf][W::place(row, piece)] = qp[x];
+            if (piece == 0) lse_lds[buf][row] = neg[x];
+        }
+        if (r0 + W::ROWS < R) fetch(r0 + W::ROWS);
+        // (LDS only.  One meeting a stage: whoever writes a buffer again has met those that have read it)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+        const int rows = min(W::ROWS, R - r0);
+        for (int t0 = 0; t0 < rows; t0 += 32) {
+            f32x16 sc;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const uint4 qf = q_lds[W::place(t0 + col, 2 * i + half)];
+            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
-                for (int x = 0; x < TILES; ++x) sc[x] = Mfma32<T>::step(kk[x][i], qf, sc[x]);
-            }
-            const float neg = lse_lds[t0 + col];
+            for (int i = 0; i < STEPS; ++i) sc = Mfma32<T>::step(kk[i], q_lds[buf][W::place(t0 + col, 2 * i + half)], sc);
+            const float n = lse_lds[buf][t0 + col];
 #pragma unroll
-            for (int x = 0; x < TILES; ++x)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sum[x][i] += __builtin_amdgcn_exp2f(fmaf(sc[x][i], k.scale_log2, neg));
+            for (int i = 0; i < 16; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(sc[i], k.scale_log2, n));
         }
     }
     // ---- fold the columns; value i of a tile is its token 8 * (i >> 2) + 4 * half + (i & 3) ----
-#pragma unroll
-    for (int x = 0; x < TILES; ++x) {
-        const float w = fold32(sum[x], lane);
-        const int i = ((lane & 1) << 3) | ((lane & 2) << 1) | ((lane & 4) >> 1) | ((lane & 8) >> 3);
-        const int t = __shfl(tok[x], 8 * (i >> 2) + 4 * half + (i & 3));
-        if ((lane & 16) || t < 0) continue;
-        float *to = k.a.weights + bg * cap + t;
-        // (a block that is listed m times is added to m times, by the same amount each: the order changes nothing)
-        if (LISTS) unsafeAtomicAdd(to, w);
-        else *to += w;
-    }
+    const float w = fold32(sum, lane);
+    const int i = ((lane & 1) << 3) | ((lane & 2) << 1) | ((lane & 4) >> 1) | ((lane & 8) >> 3);
+    const int t = __shfl(tok, 8 * (i >> 2) + 4 * half + (i & 3));
+    if ((lane & 16) || t < 0) return;
+    float *to = k.a.weights + bg * cap + t;
+    // (a block that is listed m times is added to m times, by the same amount each: the order changes nothing)
+    if (LISTS) unsafeAtomicAdd(to, w);
+    else *to += w;
 }
 
 hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream_t st)
@@ -183,19 +176,27 @@ hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream
     const WeighKernelArgs k{s, a, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.G), kLog2e / sqrtf((float)s.D)};
     const int64_t positions = (a.sel_idx ? (int64_t)a.n_sel : (int64_t)s.max_blocks) * s.B;
     if (positions <= 0) return hipSuccess;
-#define SPECPV_WEIGH_L(T, DD, LISTS)                                                                            \
-    do {                                                                                                        \
-        const int64_t per = kWeighWaves * 32 * WeighTile<T, DD>::TILES;                                         \
-        const dim3 grid((unsigned)((positions + per - 1) / per), s.Hkv, s.batch);                               \
-        hipLaunchKernelGGL((weigh_kernel<T, DD, LISTS>), grid, dim3(64 * kWeighWaves), 0, st, k);               \
+    const int64_t rows = (int64_t)(a.nodes ? a.max_nodes : s.M) * s.G;
+    // Many wavefronts to a workgroup from 128 rows and as many tokens on as give every CU one (64 channels, half the products: several).  Many /
+    // four, us, 8 KV heads: 128 channels, 32K, 16 rows 16.0 / 14.6, 128 22.9 / 24.8, 240 31.2 / 36.8, 480 47.3 / 60.8; 8K, 64 9.1 / 8.3, 128
+    // 10.9 / 11.0, 480 21.8 / 25.7; 2K, 240 13.2 / 10.6, 480 21.4 / 23.5; 64 channels, 32K, 240 20.3 / 24.7, 8K 10.4 / 9.5; fp32, 128 channels, 32K, 64
+    // 72 / 70, 240 189 / 208, 8K 46 / 53, 2K 45 / 36; 64 channels, 32K, 240 81 / 87, 8K 40 / 28.
+    const bool many = rows >= 128 && positions * s.batch * s.Hkv >= (int64_t)(s.D == 64 ? 1024 : 256) * device_cu_count();
+#define SPECPV_WEIGH_L(T, DD, MANY, LISTS)                                                                               \
+    do {                                                                                                                 \
+        const int64_t per = WeighTile<T, DD, MANY>::WAVES * 32;                                                          \
+        const dim3 grid((unsigned)((positions + per - 1) / per), s.Hkv, s.batch);                                        \
+        hipLaunchKernelGGL((weigh_kernel<T, DD, MANY, LISTS>), grid, dim3(64 * WeighTile<T, DD, MANY>::WAVES), 0, st, k); \
     } while (0)
-#define SPECPV_WEIGH(T, DD) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, true); else SPECPV_WEIGH_L(T, DD, false); } while (0)
+#define SPECPV_WEIGH_M(T, DD, MANY) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, MANY, true); else SPECPV_WEIGH_L(T, DD, MANY, false); } while (0)
+#define SPECPV_WEIGH(T, DD) do { if (many) SPECPV_WEIGH_M(T, DD, true); else SPECPV_WEIGH_M(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {
         if (s.D == 128) SPECPV_WEIGH(bf16_t, 128); else SPECPV_WEIGH(bf16_t, 64);
     } else {
         if (s.D == 128) SPECPV_WEIGH(float, 128); else SPECPV_WEIGH(float, 64);
     }
 #undef SPECPV_WEIGH
+#undef SPECPV_WEIGH_M
 #undef SPECPV_WEIGH_L
     return hipGetLastError();
 }
