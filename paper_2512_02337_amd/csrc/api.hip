@@ -662,15 +662,22 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
     return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
 }
 
-// Splits: as many as have a place at once.
+// Splits: one workgroup to a CU.  Tiles of 32 rows, and fp32's, have place for two, which pays where the other leaves a wavefront more than
+// 16 chunks (us, one / two, 8 KV heads: 60 query tokens x 4 heads 4K 14.7 / 15.4, 16K 33.7 / 29.9, 64K 108.5 / 85.6; 16 query tokens 16K 15.3 / 16.8,
+// 64K 33.7 / 31.1; 8, 64K 23.0 / 24.7; fp32, 128 channels, 4, 16K 13.3 / 15.7, 64K 25.8 / 25.4).  Every split's partials are read again by the
+// combine kernel: no more than a chunk to every wavefront of four, and 64 (two KV heads, 64K, 32 / 64 / 128: 17.1 / 15.1 / 17.1).
+// Two also where one leaves a third of the CUs idle (20 sequences of 8K, one token: 38.4 / 34.6; of 4K, 8 tokens: 33.2 / 25.0; 12 of 8K, a
+// quarter idle: 23.2 / 26.2).
 static int64_t packed_splits(const Shape &s, int dtype, int64_t n_blocks)
 {
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
     const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype);
-    const int64_t waves = packed_waves(packed_row_tile(s, dtype), dtype == SPECPV_F32, s.D);
-    int64_t ns = packed_places(s, dtype) * (int64_t)device_cu_count() / columns;
-    if (ns > (chunks + waves - 1) / waves) ns = (chunks + waves - 1) / waves;
-    if (ns > 128) ns = 128;
+    const int64_t waves = packed_waves(packed_row_tile(s, dtype), dtype == SPECPV_F32);
+    const int64_t cus = device_cu_count();
+    int64_t ns = cus / columns;
+    if ((waves == 4 && chunks > 64 * ns) || 3 * ns * columns < 2 * cus) ns = 2 * cus / columns;
+    if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
+    if (ns > 64) ns = 64;
     return ns < 1 ? 1 : ns;
 }
 

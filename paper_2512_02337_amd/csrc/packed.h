@@ -67,18 +67,15 @@ hipError_t launch_packed_gather(const PackedShape &p, int dtype, const int32_t *
 // Context part of the attention (packed_attn.hip): part.nsplit splits of row tiles of 16 or 32.
 // Whether a chunk's 32 tokens follow each other: the whole cache, or blocks of whole chunks (rows no more than 2^26 bytes apart).
 static inline bool packed_runs(const Shape &s, bool lists) { return (!lists || s.B % 32 == 0) && s.st < ((int64_t)1 << 26); }
-// (fp32 at 128 channels has registers for 16 rows' three operands only)
+// Tiles of 16 rows where one is enough (one query token, 16 / 32, us: 16K tokens 12.1 / 13.7, 128K 30.8 / 37.1; 32 rows as two of them: 16K 13.0 /
+// 13.1, 128K 39.1 / 39.7).  (fp32 at 128 channels has registers for 16 rows' three operands only)
 static inline int packed_row_tile(const Shape &s, int dtype) { return s.M * s.G <= 16 || (dtype == SPECPV_F32 && s.D == 128) ? 16 : 32; }
 static inline int packed_row_tiles(const Shape &s, int dtype) { return (s.M * s.G + packed_row_tile(s, dtype) - 1) / packed_row_tile(s, dtype); }
-// Wavefronts of a workgroup, each with every so-manieth chunk of its split; and workgroups that a CU has room for.  Tiles of 16 rows: three
-// wavefronts a SIMD, all in one workgroup, so that a split more does not mean a partial more.  (Six of them: a SIMD gets two of one workgroup and
-// none of the next, and half of the workgroups wait: one token over 128K, 31.3 us where this takes 27.0.)
-__host__ __device__ constexpr int packed_waves(int rt, bool f32, int D) { return rt == 16 && !f32 ? (D == 64 ? 16 : 12) : 4; }
-static inline int packed_places(const Shape &s, int dtype)
-{
-    if (dtype == SPECPV_F32) return s.D == 64 && s.M * s.G <= 16 ? 3 : 2;
-    return packed_row_tile(s, dtype) == 16 ? 1 : (s.D == 64 ? 3 : 2);
-}
+// Wavefronts of a workgroup, each with every so-manieth chunk of its split.  16 rows: eight, so that one workgroup to a CU, hence no more
+// partials than the combine kernel reads quickly, has bytes enough under way.  (us, 8 KV heads of 128 channels, one query token: 4 / 8 / 12
+// wavefronts with a chunk more under way, 8K tokens 10.0 / 9.9 / 10.6, 32K 14.6 / 14.1 / 14.9, 128K 32.0 / 30.7 / 30.9; 8 / 12 so, 2K 7.6 / 7.8, 8K
+// 9.7 / 9.8, 32K 12.9 / 13.5, 128K 29.1 / 29.8; 64 channels, 8K 8.0 / 8.3, 128K 18.5 / 17.7.)
+__host__ __device__ constexpr int packed_waves(int rt, bool f32) { return rt == 16 && !f32 ? 8 : 4; }
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st);
 
 }  // namespace specpv

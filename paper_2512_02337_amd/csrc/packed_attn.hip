@@ -6,7 +6,8 @@
 // A wavefront works for itself: the K codes of a chunk are its A operand as they come from memory (a lane holds half of a
 // token's row; which channels a step of the product takes does not matter as long as Q's are the same), V goes through a
 // piece of LDS of its own as bf16, because its operand has tokens where memory has channels: the transposing LDS reads turn it.
-// The next two chunks' codes, 35 bytes a lane each, are under way while one is worked on.
+// The next chunk's codes, 35 bytes a lane, are under way while one is worked on.  (Two of them: 13.8 us for 12.9 over 32K tokens, 30.5 for
+// 29.1 over 128K, 50.6 for 49.0 over 32 sequences of 8K: a split's end reads more for nothing, and there are wavefronts enough.)
 #include "packed.h"
 #include "attn_mfma.h"
 
@@ -82,7 +83,7 @@ template <int D> struct RowTile<16, D> {
 };
 
 template <typename T, int D, int RT, bool RUN>
-__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4, D), RT == 16 && sizeof(T) == 2 ? (D == 64 ? 4 : 3) : 2) void packed_attn_kernel(PackedAttnArgs a)
+__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), 2) void packed_attn_kernel(PackedAttnArgs a)
 {
     typedef RowTile<RT, D> Tile;
     typedef typename Tile::Acc Acc;
@@ -90,8 +91,7 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4, D), RT == 16 
     constexpr int PARTS = 64 / RT, SHARE = D / PARTS, STEPS = SHARE / 8;   // lanes of a column; their channels, and steps of the product
     constexpr int KWORDS = SHARE / 8;                 // 4-byte words of K codes of a lane and tile
     constexpr int OT = D / RT, VLOADS = D / 64;
-    constexpr int RING = N == 1 && RUN ? 3 : 2;              // chunks in registers: this one and those under way
-    constexpr int WAVES = packed_waves(RT, N > 1, D);
+    constexpr int WAVES = packed_waves(RT, N > 1);
     constexpr bool STREAM = RT == 16 && N == 1;       // codes past the caches: they are read once (one row tile)
     constexpr int VROW = D * 2;                       // bytes of a V row in LDS
     constexpr int VALUES = OT * REGS;                 // results of a lane
@@ -337,23 +337,19 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4, D), RT == 16 
     };
 
     if (c0 + wave < c1) {
-        Codes ring[RING];
+        Codes even, odd;   // (in turn, so that no registers move)
         int c = c0 + wave;
-#pragma unroll
-        for (int x = 0; x < RING - 1; ++x) fetch(tokens_of(c + x * WAVES), ring[x]);
-        Tokens next = tokens_of(c + (RING - 1) * WAVES);
+        fetch(tokens_of(c), even);
+        Tokens next = tokens_of(c + WAVES);
         for (;;) {
-            bool done = false;
-#pragma unroll
-            for (int x = 0; x < RING; ++x) {   // (in turn, so that no registers move)
-                const Tokens now = next;
-                next = tokens_of(c + RING * WAVES);
-                fetch(now, ring[(x + RING - 1) % RING]);
-                work(ring[x]);
-                c += WAVES;
-                if (c >= c1) { done = true; break; }
-            }
-            if (done) break;
+            fetch(next, odd);
+            next = tokens_of(c + 2 * WAVES);
+            work(even);
+            if ((c += WAVES) >= c1) break;
+            fetch(next, even);
+            next = tokens_of(c + 2 * WAVES);
+            work(odd);
+            if ((c += WAVES) >= c1) break;
         }
     }
     // ---- the wavefronts' results into one: all of them to LDS, and each wavefront merges and stores every so-manieth four channels ----
@@ -408,8 +404,8 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
 #define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
     do {                                                                                                                                \
-        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4, DD)), 0, st, a);                \
-        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4, DD)), 0, st, a); \
+        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4)), 0, st, a);                \
+        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4)), 0, st, a); \
     } while (0)
 #define SPECPV_ATTN(T, DD) do { if (run) SPECPV_ATTN_R(T, DD, true); else SPECPV_ATTN_R(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {
