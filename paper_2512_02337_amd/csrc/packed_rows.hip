@@ -152,8 +152,11 @@ hipError_t launch_pack(const Shape &src, int dtype, const PackedShape &p, const 
     if (!a.kmax) k.unit = 64;
     const int64_t most = (k.capacity + k.unit - 1) / k.unit, rows = ((int64_t)a.max_rows + k.unit - 2) / k.unit + 1;
     const int64_t units = 2 * (rows < most ? rows : most);
-    // long blocks, or too few of them to give every SIMD a wavefront: a workgroup to each
-    const bool wide = k.unit > 64;
+    // A workgroup to a block where that is no more than eight workgroups to a CU, or the blocks are long (us, wavefronts / workgroups, 8 heads, bf16:
+    // blocks of 32, 64 rows 11.3 / 10.0, 1K 14.6 / 12.3, 2K 15.9 / 14.8, 4K 19.6 / 20.6, 32K 61.7 / 94.9; of 64, 64 rows 14.4 / 10.5, 1K 18.3 / 12.7, 8K
+    // 31.4 / 29.1, 32K 61.6 / 72.7; of 128, 1K 28.0 / 15.0, 32K 61.7 / 63.1, 128K 245 / 237; of 256, 128K 250 / 233; fp32, of 64, 4K 34.5 / 26.2.)  Blocks
+    // of 16 are a pass of eight loads or less for a wavefront by itself (1K rows 11.9 / 12.8).
+    const bool wide = k.unit > 64 || (k.unit > 16 && units * p.s.Hkv * p.s.batch <= 8 * (int64_t)device_cu_count());
     const dim3 grid((unsigned)(wide ? units : (units + 3) / 4), p.s.Hkv, p.s.batch);
 #define SPECPV_PACK(T, DD)                                                                                   \
     do {                                                                                                     \
