@@ -514,6 +514,8 @@ hipError_t launch_evict(const Shape &s, const Shape &d, int dtype, const EvictAr
     const int64_t cap = (int64_t)s.max_blocks * s.B;
     const EvictKernelArgs k{s, d, a, cap, (int64_t)d.max_blocks * d.B, pick_chunks(cap)};
     const dim3 one(s.Hkv, s.batch), hists((unsigned)(k.chunks * kChunk / kHistTokens), s.Hkv, s.batch), chunks((unsigned)k.chunks, s.Hkv, s.batch), threads(64 * kPickWaves);
+    // (us, whole call, 8 heads, a quarter kept: 4K with four keys a thread / sixteen / by many workgroups 10.8 / 14.8 / 21.3; 8K, sixteen / many
+    // 17.0 / 24.3, 16K 21.5 / 26.8; 64 heads, 16K 64.6 / 70.1)
     if (cap <= 4096) {
         hipLaunchKernelGGL(pick_kernel<4>, one, threads, 0, st, k);
     } else if (cap <= kPickMost) {
@@ -528,7 +530,9 @@ hipError_t launch_evict(const Shape &s, const Shape &d, int dtype, const EvictAr
     const int elem = dtype == SPECPV_BF16 ? 2 : 4, row = s.D * elem, per = 4 * 256 / (row / 16);
     const int64_t rows = a.new_weights ? k.dcap : (int64_t)a.ns + a.k + a.nr;
     const dim3 grid((unsigned)((rows + per - 1) / per), s.Hkv, s.batch);
-    const bool stream = (int64_t)s.batch * s.Hkv * rows * row * 4 >= ((int64_t)64 << 20);   // bytes read and written
+    // Past the caches where the rows would only push each other out of them (bytes read and written; plain / past them, whole call, us: 64 MB 35.7 /
+    // 36.4, 96 MB 43.6 / 42.8, 128 MB 54.6 / 49.9, 256 MB 79.5 / 72.1)
+    const bool stream = (int64_t)s.batch * s.Hkv * rows * row * 4 > ((int64_t)64 << 20);
 #define SPECPV_MOVE(ROW)                                                                                     \
     do {                                                                                                     \
         if (stream) hipLaunchKernelGGL((move_kernel<ROW, true>), grid, dim3(256), 0, st, k, elem);           \
