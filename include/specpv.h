@@ -351,7 +351,7 @@ int specpv_pack_tokens(const specpv_kv *src, const int32_t *src_begin, const int
  * theirs (all tree nodes that are keys only lie in kd / vd, in the shared dtype).  One workspace, zero-filled once, serves
  * packed and ordinary calls if it has the larger size.  fp32 queries and weights are taken in full (24 bits); bf16 weights are
  * rounded to bf16 in front of the product with V, as by the ordinary calls, and at head dim 128 the pieces' results travel as fp16 like theirs:
- * V entries beyond +-65504 are clamped, and results below 2^-14 are exact to 2^-25. */
+ * V entries beyond +-65504 are clamped, and results below 2^-14 are exact to 2^-25.  workspace: 16-byte aligned. */
 size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tree *tree, const specpv_select_cfg *cfg);
 int specpv_packed_select_blocks(const specpv_packed_kv *kv, const specpv_tree *tree, const void *kmax, const void *kmin,
                                 const specpv_select_cfg *cfg, int32_t *sel_idx, int32_t *sel_count, float *scores,
@@ -388,7 +388,7 @@ int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, cons
  * Keys keep the positions they were rotated for: attention over dst is attention over the kept tokens.  dst shares batch, Hkv, D and
  * dtype with kv, has room for n tokens, and none of its memory (ctx_len included) is kv's: one spare cache serves all layers in turn.
  * Summaries and kept-block lists of dst are the caller's to rebuild.
- * Workspace: specpv_evict_workspace_bytes(kv), zero-filled once (specpv_workspace_bytes), shared with other calls like any. */
+ * Workspace: specpv_evict_workspace_bytes(kv), 16-byte aligned, zero-filled once (specpv_workspace_bytes), shared with other calls like any. */
 size_t specpv_evict_workspace_bytes(const specpv_kv *kv);
 int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sink, int32_t n_recent, int32_t k_tokens,
                         const specpv_kv *dst, float *dst_weights, int32_t *keep_idx,

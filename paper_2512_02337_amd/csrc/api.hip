@@ -993,6 +993,7 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
     const PackedShape p = make_packed(kv, tree);
     const Shape &s = p.s;
+    if ((uintptr_t)workspace & 15) return SPECPV_EINVAL;
     if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, 1)) return SPECPV_EWORKSPACE;
     int64_t ns = packed_splits(s, kv->dtype, sel_idx ? n_sel : s.max_blocks);
     while (ns > 1 && packed_bytes(s, kv->dtype, ns) > workspace_bytes) --ns;
@@ -1049,6 +1050,7 @@ int specpv_evict_tokens(const specpv_kv *kv, const float *weights, int32_t n_sin
     const int64_t n = (int64_t)n_sink + n_recent + k_tokens;
     if (n < 1 || n > (int64_t)dst->max_blocks * dst->block_size) return SPECPV_EINVAL;
     if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
+    if ((uintptr_t)workspace & 15) return SPECPV_EINVAL;
     if (!workspace || workspace_bytes < specpv_evict_workspace_bytes(kv)) return SPECPV_EWORKSPACE;
     const EvictArgs a{n_sink, n_recent, k_tokens, weights, dst_weights, keep_idx, (uint32_t *)((char *)workspace + kArriveBytes)};
     const hipError_t e = launch_evict(make_shape(kv, nullptr), make_shape(dst, nullptr), kv->dtype, a, (hipStream_t)stream);

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackKernelArgs k)
     const int g = blockIdx.y, b = blockIdx.z;
     const int at = WIDE ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave;
     const bool values = at & 1;
-    const int L = k.src.ctx_len[b];
+    const int L = (int)min((int64_t)k.src.ctx_len[b], (int64_t)k.src.max_blocks * k.src.B);
     const int64_t sb = k.a.src_begin ? k.a.src_begin[b] : 0, db = k.a.dst_begin ? k.a.dst_begin[b] : 0;
     int64_t n = k.a.n_rows ? k.a.n_rows[b] : (k.a.src_rows ? (int64_t)k.a.max_rows : (int64_t)L - sb);
     if (n > k.a.max_rows) n = k.a.max_rows;

@@ -120,3 +120,9 @@ def test_binding_refuses():
         specpv.PackedKV(u8(1, 2, 64, 64).float(), u8(1, 2, 64, 64), u8(1, 2, 64, 4), u8(1, 2, 64, 4), one, 16)
     with pytest.raises(ValueError):
         specpv.PackedKV(u8(1, 2, 64, 64), u8(1, 2, 64, 64), u8(1, 2, 64, 4), u8(1, 2, 64, 4), one, 16, dtype=torch.float16)
+
+
+def test_workspaces_off_their_alignment():
+    lib = specpv.load()
+    assert lib.specpv_packed_verify_attn(B(_packed()), B(_tree()), None, None, 0, vp(0x300), None, vp(0x8008), 1 << 40, None) == -1
+    assert lib.specpv_evict_tokens(B(_kv()), vp(0x100), 4, 8, 20, B(_kv(k=0x11000, v=0x12000, ctx_len=0x13000)), vp(0x200), vp(0x300), vp(0x8004), 1 << 30, None) == -1

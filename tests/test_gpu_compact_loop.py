@@ -166,3 +166,33 @@ def test_nothing_is_allocated(gpu_lib):
     loop.run()
     torch.cuda.synchronize()
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+
+
+def test_two_graphs_in_one_workspace(gpu_lib):
+    """Graphs of different shapes that share a workspace, replayed in turn, and an eager call between them."""
+    sp = gpu_lib
+    loops = [Loop(sp), Loop(sp, 20000, (2, 33, 9000))]
+    ws = loops[0].ws if loops[0].ws.numel() > loops[1].ws.numel() else loops[1].ws
+    want, graphs = [], []
+    for loop in loops:
+        loop.ws = ws
+        want.append([t.clone() for t in loop.run()])
+    torch.cuda.synchronize()
+    for loop in loops:
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            loop.run()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs = loop.run()
+        loop.outs = outs
+    for i in range(3):
+        for j in (0, 1, 1, 0):
+            for t in loops[j].outs:
+                t.zero_() if t is not loops[j].packed.ctx_len else None
+            graphs[j].replay()
+        loops[i & 1].run()
+        torch.cuda.synchronize()
+        for loop, w in zip(loops, want):
+            assert all(torch.equal(a, b) for a, b in zip(loop.outs, w)), i

@@ -159,3 +159,14 @@ def test_binding_refuses(gpu_lib):
         sp.specpv_pack_tokens(src, h)                        # fp32 rows, a cache for bf16
     with pytest.raises(ValueError):
         sp.PackedKV(h.k, h.v, h.k_scale[:, :, ::2], h.v_scale[:, :, ::2], h.ctx_len, 16)
+
+
+@pytest.mark.parametrize("dtype,D,M,Hq,Hkv,lens", [(torch.bfloat16, 128, 60, 8, 2, [40000]), (torch.bfloat16, 64, 1, 4, 1, [20000]), (torch.float32, 64, 9, 8, 2, [30001]),
+                                                   (torch.bfloat16, 128, 2, 16, 8, list(range(1, 300, 15))), (torch.float32, 64, 9, 16, 8, list(range(0, 300, 15)))])
+def test_splits_of_every_kind(gpu_lib, dtype, D, M, Hq, Hkv, lens):
+    """One workgroup a CU and two, the most splits that there are, and a number of columns that leaves a third of the CUs idle."""
+    sp = gpu_lib
+    T = -(-max(lens) // 64) * 64
+    h, k, v = ref.cache(sp, len(lens), Hkv, T, D, 64, dtype, seed=M, lens=lens)
+    tree, tv, parent = _tree(sp, len(lens), M, 0, Hq, Hkv, D, dtype, M + D)
+    check(sp, h, (k, v), tree, tv, parent)

@@ -194,3 +194,39 @@ def test_gather(gpu_lib, dtype, D, Bk, layout, gap):
         for o, w in zip(out, (k, v)):
             assert np.array_equal(o[b, :, :lens[b]].double().cpu().numpy(), w[b, :, :lens[b]]) and not o[b, :, lens[b]:].any()
     assert ln.tolist() == lens
+
+
+@pytest.mark.parametrize("dtype,Bk", [(torch.bfloat16, 32), (torch.float32, 48), (torch.bfloat16, 64), (torch.float32, 128)])
+def test_more_blocks_than_workgroups(gpu_lib, dtype, Bk):
+    """A long prompt in two calls, cut inside a block: codes as from a cache of blocks of 16, summaries as from block_summarize."""
+    sp = gpu_lib
+    n = 9000
+    src, _, _ = _source(sp, 2, 4, n, 64, dtype, "bthd", 6, [n, n - 700])
+    T = -(-n // 384) * 384
+    a, b = Target(sp, 2, 4, T, 64, Bk, dtype), Target(sp, 2, 4, T, 64, 16, dtype)
+    cut = torch.tensor([4501, 4501], dtype=torch.int32, device="cuda")
+    got = [torch.full(a.h.summary_shape(), 7.0, dtype=dtype, device="cuda") for _ in "xn"]
+    want = [torch.full(a.h.summary_shape(), 7.0, dtype=dtype, device="cuda") for _ in "xn"]
+    sp.specpv_pack_tokens(src, a.h, n_rows=cut, kmax=got[0], kmin=got[1])
+    sp.specpv_pack_tokens(src, a.h, dst_begin=cut, src_begin=cut, kmax=got[0], kmin=got[1])
+    sp.specpv_pack_tokens(src, b.h)
+    for x, y in zip(a.host(), b.host()):
+        assert np.array_equal(x, y)
+    whole = [torch.zeros((2, T, 4, 64), dtype=dtype, device="cuda") for _ in "kv"]
+    for x, y in zip(whole, (src.k, src.v)):
+        x[:, :n] = y if y.shape[1] == n else y.permute(0, 2, 1, 3)
+    sp.specpv_block_summarize(sp.KV(whole[0], whole[1], src.ctx_len, Bk, layout="bthd"), 0, -1, *want)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_length_beyond_the_source(gpu_lib):
+    """A source whose length claims more rows than it has room for gives those that it has."""
+    sp = gpu_lib
+    src, k, v = _source(sp, 1, 2, 16, 64, torch.bfloat16, "bhtd", 8, [40])
+    t = Target(sp, 1, 2, 48, 64, 16, torch.bfloat16)
+    want = _expect(t.host(), (k, v), [(0, i, i) for i in range(16)])
+    sp.specpv_pack_tokens(src, t.h, max_rows=40)
+    _same(t, want)
+    rows = torch.tensor([[20, 15, 16, 39]], dtype=torch.int32, device="cuda")
+    sp.specpv_pack_tokens(src, t.h, src_rows=rows, dst_begin=torch.tensor([30], dtype=torch.int32, device="cuda"))
+    _same(t, _expect(want, (k, v), [(0, 31, 15)]))

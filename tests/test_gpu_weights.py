@@ -117,3 +117,21 @@ def test_binding_refuses(gpu_lib):
                 (lse, w, nodes[0], n)):
         with pytest.raises(ValueError):
             sp.specpv_accumulate_weights(c.kv, c.tree, *bad)
+
+
+@pytest.mark.parametrize("dtype,D,batch,Hq,M,layout", [(torch.bfloat16, 128, 4, 6, 43, "bhtd"), (torch.bfloat16, 128, 4, 16, 40, "bthd"), (torch.float32, 128, 4, 8, 33, "bhtd"),
+                                                       (torch.bfloat16, 64, 16, 6, 43, "bthd"), (torch.float32, 64, 16, 10, 40, "bhtd")])
+def test_many_rows_of_many_tokens(gpu_lib, dtype, D, batch, Hq, M, layout):
+    """128 rows and more for room enough to give every CU tokens, most of it not used; whole caches, some rows, and lists."""
+    T = 8192
+    c = Case(gpu_lib, dtype, D, Hq, 2, M, 16, [T - 1, 100, 0, 33] + [5] * (batch - 4), layout, seed=M + D)
+    c.check(gpu_lib)
+    g = torch.Generator().manual_seed(7)
+    nodes = torch.randint(-2, M + 2, (batch, M + 3), generator=g).to(torch.int32).cuda()
+    n = torch.randint(0, M + 4, (batch,), generator=g).to(torch.int32)
+    n[0] = M + 3
+    idx = torch.randint(-1, T // 16 + 1, (batch, 2, T // 16), generator=g).to(torch.int32)
+    idx[1:, :, 1::2] = 0
+    cnt = torch.randint(0, T // 16 + 1, (batch, 2), generator=g).to(torch.int32)
+    c.check(gpu_lib, nodes, n.cuda())
+    c.check(gpu_lib, idx=idx.cuda(), cnt=cnt.cuda())
