@@ -55,13 +55,11 @@ __device__ __forceinline__ float fold32(const float (&v)[16], int lane)
     return d + __shfl_xor(d, 16);
 }
 
-// WAVES: 4, or as many as a CU takes (MANY).  A stage's query rows are found and fetched by all of a workgroup's threads, on their way
-// to registers while the stage before is worked on; many rows are cheaper for many wavefronts at once, but one workgroup to a CU
-// has nobody to compute while it reads its K rows (launch_weigh).
-template <typename T, int D, bool MANY> struct WeighTile {
+// A workgroup has WAVES wavefronts (launch_weigh).  A stage's query rows are found and fetched by all of its threads, on their way to
+// registers while the stage before is worked on; what rows cost is the less, the more wavefronts they are fetched for.
+template <typename T, int D, int WAVES> struct WeighTile {
     static constexpr int E = Elem<T>::kPerVec, STEPS = D / (2 * E);        // channels of a lane's 16 bytes; products of a tile
     static constexpr int PIECES = D / E;                                   // 16-byte pieces of a row
-    static constexpr int WAVES = !MANY ? 4 : (STEPS * 4 > 32 ? 8 : 16);    // (K rows: 32 registers, or 64)
     static constexpr int MINE = PIECES == 32 ? 4 : 2;                      // pieces of a stage that a thread brings
     static constexpr int ROWS = MINE * 64 * WAVES / PIECES;                // query rows of a stage
     static_assert(ROWS % 32 == 0, "whole tiles");
@@ -72,11 +70,11 @@ template <typename T, int D, bool MANY> struct WeighTile {
     }
 };
 
-template <typename T, int D, bool MANY, bool LISTS>
-__global__ __launch_bounds__((64 * WeighTile<T, D, MANY>::WAVES)) void weigh_kernel(WeighKernelArgs k)
+template <typename T, int D, int WAVES, bool LISTS>
+__global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
 {
-    typedef WeighTile<T, D, MANY> W;
-    constexpr int STEPS = W::STEPS, THREADS = 64 * W::WAVES;
+    typedef WeighTile<T, D, WAVES> W;
+    constexpr int STEPS = W::STEPS, THREADS = 64 * WAVES;
     __shared__ uint4 q_lds[2][W::ROWS * W::PIECES];
     __shared__ float lse_lds[2][W::ROWS];   // -lse * log2 e; -inf: no such row
     const Shape &s = k.s;
@@ -88,7 +86,7 @@ __global__ __launch_bounds__((64 * WeighTile<T, D, MANY>::WAVES)) void weigh_ker
     const int nb = (int)k.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
     int span = L;   // positions that there are
     if (LISTS) span = max(min(k.a.sel_count[bg], k.a.n_sel), 0) * s.B;
-    const int p0 = (int)blockIdx.x * (W::WAVES * 32);
+    const int p0 = (int)blockIdx.x * (WAVES * 32);
     if (p0 >= span || L == 0) return;
     // ---- the wavefront's K rows ----
     int tok = -1;
@@ -177,26 +175,36 @@ hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream
     const int64_t positions = (a.sel_idx ? (int64_t)a.n_sel : (int64_t)s.max_blocks) * s.B;
     if (positions <= 0) return hipSuccess;
     const int64_t rows = (int64_t)(a.nodes ? a.max_nodes : s.M) * s.G;
-    // Many wavefronts to a workgroup from 128 rows and as many tokens on as give every CU one (64 channels, half the products: several).  Many /
-    // four, us, 8 KV heads: 128 channels, 32K, 16 rows 16.0 / 14.6, 128 22.9 / 24.8, 240 31.2 / 36.8, 480 47.3 / 60.8; 8K, 64 9.1 / 8.3, 128
-    // 10.9 / 11.0, 480 21.8 / 25.7; 2K, 240 13.2 / 10.6, 480 21.4 / 23.5; 64 channels, 32K, 240 20.3 / 24.7, 8K 10.4 / 9.5; fp32, 128 channels, 32K, 64
-    // 72 / 70, 240 189 / 208, 8K 46 / 53, 2K 45 / 36; 64 channels, 32K, 240 81 / 87, 8K 40 / 28.
-    const bool many = rows >= 128 && positions * s.batch * s.Hkv >= (int64_t)(s.D == 64 ? 1024 : 256) * device_cu_count();
-#define SPECPV_WEIGH_L(T, DD, MANY, LISTS)                                                                               \
+    // Eight wavefronts from 64 rows on where every CU gets tokens for eight, in bf16 from 192 rows on (there the rows themselves, brought by more
+    // threads, are what matters).  (us, 8 KV heads, 4 / 8: bf16, 128 channels, 64 rows 2K 5.2 / 5.5, 4K 5.3 / 6.0, 8K 7.9 / 6.7, 128K 68.2 / 64.1;
+    // 240 rows 2K 10.6 / 10.0, 8K 16.0 / 12.0, 32K 36.6 / 30.3; 480 rows 2K 23.4 / 18.3; 64 channels, 64 rows 2K 4.1 / 4.3, 8K 4.9 / 4.3,
+    // 240 rows 64K 42.5 / 35.7; fp32, 128 channels, 64 rows 2K 11.9 / 15.6, 8K 18.7 / 17.8, 240 rows 2K 35.4 / 44.7, 8K 52.3 / 47.0; 64 channels, 240 rows
+    // 8K 28.3 / 25.4.)  Sixteen for bf16 at 128 channels where every CU gets tokens for those (8 / 16: 128 rows, 8K 8.6 / 10.4, 16K 12.5 / 11.9; 240, 16K
+    // 17.3 / 15.9, 32K 30.3 / 29.4; 480, 8K 18.9 / 21.5, 32K 48.9 / 45.1; 64 channels, 240, 64K 35.7 / 36.2; fp32, 64 channels, 128, 32K 46.9 / 47.9): one such
+    // workgroup to a CU has nobody to compute while it reads its K rows, but reads each fragment of Q for sixteen.
+    const int64_t each = positions * s.batch * s.Hkv / device_cu_count();   // tokens of a CU
+    const bool wide = dtype == SPECPV_BF16 && s.D == 128 && rows >= 128 && each >= 512;
+    const bool many = (rows >= 64 && each >= 256) || (dtype == SPECPV_BF16 && rows >= 192);
+#define SPECPV_WEIGH_L(T, DD, WAVES, LISTS)                                                                              \
     do {                                                                                                                 \
-        const int64_t per = WeighTile<T, DD, MANY>::WAVES * 32;                                                          \
-        const dim3 grid((unsigned)((positions + per - 1) / per), s.Hkv, s.batch);                                        \
-        hipLaunchKernelGGL((weigh_kernel<T, DD, MANY, LISTS>), grid, dim3(64 * WeighTile<T, DD, MANY>::WAVES), 0, st, k); \
+        const dim3 grid((unsigned)((positions + WAVES * 32 - 1) / (WAVES * 32)), s.Hkv, s.batch);                        \
+        hipLaunchKernelGGL((weigh_kernel<T, DD, WAVES, LISTS>), grid, dim3(64 * WAVES), 0, st, k);                       \
     } while (0)
-#define SPECPV_WEIGH_M(T, DD, MANY) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, MANY, true); else SPECPV_WEIGH_L(T, DD, MANY, false); } while (0)
-#define SPECPV_WEIGH(T, DD) do { if (many) SPECPV_WEIGH_M(T, DD, true); else SPECPV_WEIGH_M(T, DD, false); } while (0)
+#define SPECPV_WEIGH_W(T, DD, WAVES) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, WAVES, true); else SPECPV_WEIGH_L(T, DD, WAVES, false); } while (0)
+#define SPECPV_WEIGH(T, DD)                                                                                              \
+    do {                                                                                                                 \
+        if constexpr (sizeof(T) == 2 && DD == 128) {                                                                     \
+            if (wide) { SPECPV_WEIGH_W(T, DD, 16); break; }                                                              \
+        }                                                                                                                \
+        if (many) SPECPV_WEIGH_W(T, DD, 8); else SPECPV_WEIGH_W(T, DD, 4);                                               \
+    } while (0)
     if (dtype == SPECPV_BF16) {
         if (s.D == 128) SPECPV_WEIGH(bf16_t, 128); else SPECPV_WEIGH(bf16_t, 64);
     } else {
         if (s.D == 128) SPECPV_WEIGH(float, 128); else SPECPV_WEIGH(float, 64);
     }
 #undef SPECPV_WEIGH
-#undef SPECPV_WEIGH_M
+#undef SPECPV_WEIGH_W
 #undef SPECPV_WEIGH_L
     return hipGetLastError();
 }

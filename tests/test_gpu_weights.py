@@ -119,7 +119,7 @@ def test_binding_refuses(gpu_lib):
             sp.specpv_accumulate_weights(c.kv, c.tree, *bad)
 
 
-@pytest.mark.parametrize("dtype,D,batch,Hq,M,layout", [(torch.bfloat16, 128, 4, 6, 43, "bhtd"), (torch.bfloat16, 128, 4, 16, 40, "bthd"), (torch.float32, 128, 4, 8, 33, "bhtd"),
+@pytest.mark.parametrize("dtype,D,batch,Hq,M,layout", [(torch.bfloat16, 128, 4, 6, 43, "bhtd"), (torch.bfloat16, 128, 8, 16, 40, "bthd"), (torch.float32, 128, 4, 8, 33, "bhtd"),
                                                        (torch.bfloat16, 64, 16, 6, 43, "bthd"), (torch.float32, 64, 16, 10, 40, "bhtd")])
 def test_many_rows_of_many_tokens(gpu_lib, dtype, D, batch, Hq, M, layout):
     """128 rows and more for room enough to give every CU tokens, most of it not used; whole caches, some rows, and lists."""
