@@ -662,23 +662,26 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
     return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
 }
 
-// Splits: one workgroup to a CU.  Tiles of 32 rows, and fp32's, have place for two, which pays where the other leaves a wavefront more than
-// 16 chunks (us, one / two, 8 KV heads: 60 query tokens x 4 heads 4K 14.7 / 15.4, 16K 33.7 / 29.9, 64K 108.5 / 85.6; 16 query tokens 16K 15.3 / 16.8,
-// 64K 33.7 / 31.1; 8, 64K 23.0 / 24.7; fp32, 128 channels, 4, 16K 13.3 / 15.7, 64K 25.8 / 25.4).  Every split's partials are read again by the
-// combine kernel: no more than a chunk to every wavefront of four, and 64 (two KV heads, 64K, 32 / 64 / 128: 17.1 / 15.1 / 17.1).
-// Two also where one leaves a third of the CUs idle (20 sequences of 8K, one token: 38.4 / 34.6; of 4K, 8 tokens: 33.2 / 25.0; 12 of 8K, a
-// quarter idle: 23.2 / 26.2).
-static int64_t packed_splits(const Shape &s, int dtype, int64_t n_blocks)
+// Splits, and the wavefronts of a workgroup, each with every so-manieth chunk of its split: one workgroup to a CU, so that there are no more
+// partials for the combine kernel to read than that takes.  Eight wavefronts (two a SIMD) where they get four chunks each, and always for bf16 tiles of 16
+// rows; else four, whose results are merged sooner.  (us, 8 KV heads, 4 / 8: 60 query tokens x 4 heads 2K 11.4 / 12.0, 4K 13.7 / 13.5, 16K 33.7 / 27.6, 64K
+// 108.5 / 83.3; 30, 4K 10.9 / 11.3, 16K 21.3 / 18.9; 8, 16K 12.4 / 12.6, 64K 23.0 / 20.4; fp32, 128 channels, 4, 2K 8.1 / 8.8, 16K 12.9 / 13.5, 64K 25.8 / 22.8; 16,
+// 2K 9.6 / 10.3, 16K 23.7 / 21.5; bf16, one token, 2K 7.8 / 7.5, 8K 10.0 / 9.9, 32K 14.6 / 14.1, 128K 32.0 / 30.7, and 12: 8.0, 10.6, 14.9, 30.9.)
+// Where one workgroup to a CU leaves a third of the CUs idle, twice as many, of four wavefronts where there are such (20 sequences of 8K, one token: 38.4 /
+// 34.6; of 4K, 8 tokens: 33.2 / 25.0; 12 of 8K, a quarter idle: 23.2 / 26.2).  No more than a split to four chunks, and 64 (two KV heads, 64K, 32 / 64 / 128:
+// 17.1 / 15.1 / 17.1).
+struct PackedPlan { int64_t ns; int waves; };
+static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks)
 {
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
-    const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype);
-    const int64_t waves = packed_waves(packed_row_tile(s, dtype), dtype == SPECPV_F32);
-    const int64_t cus = device_cu_count();
+    const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype), cus = device_cu_count();
     int64_t ns = cus / columns;
-    if ((waves == 4 && chunks > 64 * ns) || 3 * ns * columns < 2 * cus) ns = 2 * cus / columns;
+    const bool idle = 3 * ns * columns < 2 * cus, few = dtype == SPECPV_BF16 && packed_row_tile(s, dtype) == 16;
+    const int waves = few || (!idle && chunks >= 32 * ns) ? 8 : 4;
+    if (idle) ns = 2 * cus / columns;
     if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
     if (ns > 64) ns = 64;
-    return ns < 1 ? 1 : ns;
+    return {ns < 1 ? 1 : ns, waves};
 }
 
 }  // namespace specpv
@@ -959,10 +962,10 @@ size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tr
     if (!tree) return kArriveBytes + 256;
     if (check_tree(&plain, tree, false) != SPECPV_OK) return 0;
     const Shape s = make_shape(&plain, tree);
-    size_t need = packed_bytes(s, kv->dtype, packed_splits(s, kv->dtype, s.max_blocks));
+    size_t need = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, s.max_blocks).ns);
     if (cfg) {
         const int64_t n_sel = (int64_t)cfg->n_sink_blocks + cfg->k_blocks + cfg->n_recent_blocks + cfg->n_extra_slots;
-        const size_t lists = packed_bytes(s, kv->dtype, packed_splits(s, kv->dtype, n_sel)), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
+        const size_t lists = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, n_sel).ns), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
         if (lists > need) need = lists;
         if (scores > need) need = scores;
     }
@@ -995,13 +998,14 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     const Shape &s = p.s;
     if ((uintptr_t)workspace & 15) return SPECPV_EINVAL;
     if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, 1)) return SPECPV_EWORKSPACE;
-    int64_t ns = packed_splits(s, kv->dtype, sel_idx ? n_sel : s.max_blocks);
+    const PackedPlan plan = packed_plan(s, kv->dtype, sel_idx ? n_sel : s.max_blocks);
+    int64_t ns = plan.ns;
     while (ns > 1 && packed_bytes(s, kv->dtype, ns) > workspace_bytes) --ns;
     if ((int64_t)packed_row_tiles(s, kv->dtype) * ns > 65535) return SPECPV_ELIMIT;
     const size_t rows = (size_t)s.batch * s.Hq * ns * s.M;
     char *const at = (char *)workspace + kArriveBytes;
     const Partials part{(float *)at, (float *)(at + align_up(rows * packed_row_bytes(s, kv->dtype))), (int)ns, packed_half(s, kv->dtype) ? 1 : 0, 0, nullptr};
-    hipError_t e = launch_packed_attn(p, kv->dtype, sel_idx, sel_count, n_sel, part, (hipStream_t)stream);
+    hipError_t e = launch_packed_attn(p, kv->dtype, sel_idx, sel_count, n_sel, part, plan.waves, (hipStream_t)stream);
     if (e == hipSuccess) e = launch_combine(s, kv->dtype, part, out, lse, (hipStream_t)stream);
     return e == hipSuccess ? SPECPV_OK : fail_hip(e);
 }

@@ -71,11 +71,7 @@ static inline bool packed_runs(const Shape &s, bool lists) { return (!lists || s
 // 13.1, 128K 39.1 / 39.7).  (fp32 at 128 channels has registers for 16 rows' three operands only)
 static inline int packed_row_tile(const Shape &s, int dtype) { return s.M * s.G <= 16 || (dtype == SPECPV_F32 && s.D == 128) ? 16 : 32; }
 static inline int packed_row_tiles(const Shape &s, int dtype) { return (s.M * s.G + packed_row_tile(s, dtype) - 1) / packed_row_tile(s, dtype); }
-// Wavefronts of a workgroup, each with every so-manieth chunk of its split.  16 rows: eight, so that one workgroup to a CU, hence no more
-// partials than the combine kernel reads quickly, has bytes enough under way.  (us, 8 KV heads of 128 channels, one query token: 4 / 8 / 12
-// wavefronts with a chunk more under way, 8K tokens 10.0 / 9.9 / 10.6, 32K 14.6 / 14.1 / 14.9, 128K 32.0 / 30.7 / 30.9; 8 / 12 so, 2K 7.6 / 7.8, 8K
-// 9.7 / 9.8, 32K 12.9 / 13.5, 128K 29.1 / 29.8; 64 channels, 8K 8.0 / 8.3, 128K 18.5 / 17.7.)
-__host__ __device__ constexpr int packed_waves(int rt, bool f32) { return rt == 16 && !f32 ? 8 : 4; }
-hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st);
+hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part,
+                              int waves, hipStream_t st);   // waves: 8, or (tiles of 32 rows, and fp32) 4
 
 }  // namespace specpv

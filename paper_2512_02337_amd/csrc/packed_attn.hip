@@ -82,8 +82,8 @@ template <int D> struct RowTile<16, D> {
     static __device__ __forceinline__ float col_sum(float x) { return sum_xor32(xor16(x, true)); }
 };
 
-template <typename T, int D, int RT, bool RUN>
-__global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), 2) void packed_attn_kernel(PackedAttnArgs a)
+template <typename T, int D, int RT, bool RUN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnArgs a)
 {
     typedef RowTile<RT, D> Tile;
     typedef typename Tile::Acc Acc;
@@ -91,7 +91,6 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), 2) void pack
     constexpr int PARTS = 64 / RT, SHARE = D / PARTS, STEPS = SHARE / 8;   // lanes of a column; their channels, and steps of the product
     constexpr int KWORDS = SHARE / 8;                 // 4-byte words of K codes of a lane and tile
     constexpr int OT = D / RT, VLOADS = D / 64;
-    constexpr int WAVES = packed_waves(RT, N > 1);
     constexpr bool STREAM = RT == 16 && N == 1;       // codes past the caches: they are read once (one row tile)
     constexpr int VROW = D * 2;                       // bytes of a V row in LDS
     constexpr int VALUES = OT * REGS;                 // results of a lane
@@ -394,7 +393,8 @@ __global__ __launch_bounds__(64 * packed_waves(RT, sizeof(T) == 4), 2) void pack
     }
 }
 
-hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part, hipStream_t st)
+hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part,
+                              int waves, hipStream_t st)
 {
     const Shape &s = p.s;
     const bool run = packed_runs(s, sel_idx != nullptr);
@@ -402,10 +402,14 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
                            make_fastdiv((uint32_t)s.M), make_fastdiv((uint32_t)tiles), kLog2e / sqrtf((float)s.D)};
     const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
+#define SPECPV_ATTN_W(T, DD, R, RUN, WAVES) hipLaunchKernelGGL((packed_attn_kernel<T, DD, R, RUN, WAVES>), grid, dim3(64 * WAVES), 0, st, a)
 #define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
     do {                                                                                                                                \
-        if (rt == 16) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 16, RUN>), grid, dim3(64 * packed_waves(16, sizeof(T) == 4)), 0, st, a);                \
-        else if constexpr (sizeof(T) == 2 || DD == 64) hipLaunchKernelGGL((packed_attn_kernel<T, DD, 32, RUN>), grid, dim3(64 * packed_waves(32, sizeof(T) == 4)), 0, st, a); \
+        if (rt == 16) {                                                                                                                 \
+            if (sizeof(T) == 2 || waves == 8) SPECPV_ATTN_W(T, DD, 16, RUN, 8); else if constexpr (sizeof(T) == 4) SPECPV_ATTN_W(T, DD, 16, RUN, 4); \
+        } else if constexpr (sizeof(T) == 2 || DD == 64) {                                                                              \
+            if (waves == 8) SPECPV_ATTN_W(T, DD, 32, RUN, 8); else SPECPV_ATTN_W(T, DD, 32, RUN, 4);                                    \
+        }                                                                                                                               \
     } while (0)
 #define SPECPV_ATTN(T, DD) do { if (run) SPECPV_ATTN_R(T, DD, true); else SPECPV_ATTN_R(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {
@@ -415,6 +419,7 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     }
 #undef SPECPV_ATTN
 #undef SPECPV_ATTN_R
+#undef SPECPV_ATTN_W
     return hipGetLastError();
 }
 
