@@ -330,6 +330,8 @@ typedef struct specpv_packed_kv {
     int32_t batch, n_kv_heads, head_dim, block_size;
     int32_t max_blocks;
     specpv_dtype dtype;
+    int32_t tokens;         /* rows that the allocation has, where those are fewer than max_blocks * block_size; 0: that many.
+                               None behind them is written                                */
 } specpv_packed_kv;
 
 /* Rows of src (an ordinary cache, a chunk of a prompt, the draft's buffer) into a packed cache.  For sequence b and
@@ -338,7 +340,7 @@ typedef struct specpv_packed_kv {
  *   src_begin[b] + i;
  * n_b = n_rows[b], or where n_rows == NULL max_rows with src_rows and src->ctx_len[b] - src_begin[b] without; at most max_rows.
  * dst_begin, src_begin, n_rows (device, [batch]) may be NULL (0, 0, as above); src_rows excludes src_begin.  Source rows outside
- * 0 .. src->ctx_len[b] - 1 and tokens outside of dst (max_blocks * block_size) are left out, their places left as they were.
+ * 0 .. src->ctx_len[b] - 1 and tokens outside of dst (max_blocks * block_size, dst->tokens) are left out, their places left as they were.
  * dst->ctx_len is neither read nor written: the caller moves it on, as it does n_pending and the like.
  * kmax, kmin (both or neither; [batch, Hkv, dst max_blocks, D] in the shared dtype): the summaries (eq. 1) of the blocks of dst that
  * receive a token, of the source's keys, unrounded: of the new rows alone in a block that dst_begin[b] does not lie behind the
@@ -371,7 +373,7 @@ int specpv_packed_gather_blocks(const specpv_packed_kv *kv, const int32_t *sel_i
  *   weights[b, g, t] += sum over the rows r of exp(q_r . k_t / sqrt(D) - lse_r),
  * over the G query heads of the nodes that count: nodes [batch, max_nodes] holds n_nodes[b] query rows of the tree each (the
  * accepted path as specpv_commit_accepted takes it: 0 is the first query node, n_key_only; entries outside 0 .. Mq - 1 are ignored, one
- * that is listed twice counts twice), or, nodes == NULL, of all Mq.  With sel_idx only the tokens of the listed blocks (one listed m
+ * that is listed twice counts twice; max_nodes <= SPECPV_MAX_M), or, nodes == NULL, of all Mq.  With sel_idx only the tokens of the listed blocks (one listed m
  * times is added to m times, as the attention attends it m times).  lse [batch, Mq, Hq] is what the attention over these keys gave;
  * a row with -inf adds nothing.  Of the tree only q, M, n_q_heads and n_key_only are read; the draft's own keys have no weights.
  * weights [batch, Hkv, max_blocks * B] fp32, the caller's, zero for tokens that nothing has looked at; entries t >= L_b are left as they
@@ -386,7 +388,7 @@ int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, cons
  *   rows 0 .. of dst->k, dst->v become theirs, in that order; dst->ctx_len[b] (written) = min(L_b, n); rows behind are left as they were;
  *   dst_weights (may be NULL) [batch, Hkv, dst max_blocks * B]: their weights, zeros behind.
  * Keys keep the positions they were rotated for: attention over dst is attention over the kept tokens.  dst shares batch, Hkv, D and
- * dtype with kv, has room for n tokens, and none of its memory (ctx_len included) is kv's: one spare cache serves all layers in turn.
+ * dtype with kv, has room (memory too) for n tokens, and none of its memory (ctx_len included) is kv's: one spare cache serves all layers in turn.
  * Summaries and kept-block lists of dst are the caller's to rebuild.
  * Workspace: specpv_evict_workspace_bytes(kv), 16-byte aligned, zero-filled once (specpv_workspace_bytes), shared with other calls like any. */
 size_t specpv_evict_workspace_bytes(const specpv_kv *kv);

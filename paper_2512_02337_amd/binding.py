@@ -52,7 +52,7 @@ class _PackedKV(ctypes.Structure):
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64), ("stride_t", ctypes.c_int64),
                 ("ctx_len", ctypes.c_void_p),
                 ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("block_size", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("dtype", ctypes.c_int)]
+                ("block_size", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("dtype", ctypes.c_int), ("tokens", ctypes.c_int32)]
 
 
 class _Tree(ctypes.Structure):
@@ -259,7 +259,7 @@ class PackedKV:
             raise ValueError("ctx_len: int32 [batch]")
         self.dtype = dtype
         self.c = _PackedKV(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), sb, sh, st,
-                           _ptr(ctx_len, torch.int32, "ctx_len").value, batch, hkv, self.D, self.B, self.max_blocks, _DTYPE[dtype])
+                           _ptr(ctx_len, torch.int32, "ctx_len").value, batch, hkv, self.D, self.B, self.max_blocks, _DTYPE[dtype], min(T, self.max_blocks * self.B))
 
     def summary_shape(self):
         return (self.batch, self.Hkv, self.max_blocks, self.D)
@@ -667,6 +667,8 @@ def specpv_evict_workspace_bytes(kv):
 def specpv_evict_tokens(kv, weights, n_sink, n_recent, k_tokens, dst, keep_idx, dst_weights=None, workspace=None):
     """The first n_sink, the last n_recent and the k_tokens heaviest of the other tokens of every KV head into the KV `dst`,
     whose ctx_len is written; keep_idx int32 [batch, Hkv, n_sink + k_tokens + n_recent]; dst_weights: their weights."""
+    if keep_idx.shape[-1] > dst.T:
+        raise ValueError("dst has no memory for so many tokens")
     rc = (_native or _loaded()).evict(kv, weights, n_sink, n_recent, k_tokens, dst, keep_idx, dst_weights, workspace)
     if rc is not None:
         return _check(rc)

@@ -633,6 +633,7 @@ static int check_packed(const specpv_packed_kv *kv)
     if (kv->dtype != SPECPV_F32 && kv->dtype != SPECPV_BF16) return SPECPV_EINVAL;
     if (kv->head_dim != 64 && kv->head_dim != 128) return SPECPV_EINVAL;
     if (kv->batch < 1 || kv->n_kv_heads < 1 || kv->block_size < 1 || kv->max_blocks < 1) return SPECPV_EINVAL;
+    if (kv->tokens < 0) return SPECPV_EINVAL;
     const int64_t row = kv->head_dim / 2;
     if (kv->stride_t < row || kv->stride_t % row || kv->stride_h % row || kv->stride_b % row || kv->stride_h < 0 || kv->stride_b < 0) return SPECPV_EINVAL;
     if (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15 || ((uintptr_t)kv->k_scale | (uintptr_t)kv->v_scale) & 3) return SPECPV_EINVAL;
@@ -649,7 +650,8 @@ static specpv_kv kv_of(const specpv_packed_kv *p)
 static PackedShape make_packed(const specpv_packed_kv *p, const specpv_tree *tree)
 {
     const specpv_kv kv = kv_of(p);
-    return PackedShape{make_shape(&kv, tree), (const uint8_t *)p->k_scale, (const uint8_t *)p->v_scale};
+    const int64_t room = (int64_t)p->max_blocks * p->block_size;
+    return PackedShape{make_shape(&kv, tree), (const uint8_t *)p->k_scale, (const uint8_t *)p->v_scale, p->tokens && p->tokens < room ? p->tokens : room};
 }
 
 // fp16 partials (bf16 at 128 channels), where the tree has no nodes that are keys only: those are the combine's here, which takes

@@ -148,7 +148,7 @@ __global__ __launch_bounds__(256) void pack_kernel(PackKernelArgs k)
 
 hipError_t launch_pack(const Shape &src, int dtype, const PackedShape &p, const PackArgs &a, hipStream_t st)
 {
-    PackKernelArgs k{src, p, a, p.s.B, (int64_t)p.s.max_blocks * p.s.B};
+    PackKernelArgs k{src, p, a, p.s.B, p.rows};
     if (!a.kmax) k.unit = 64;
     const int64_t most = (k.capacity + k.unit - 1) / k.unit, rows = ((int64_t)a.max_rows + k.unit - 2) / k.unit + 1;
     const int64_t units = 2 * (rows < most ? rows : most);

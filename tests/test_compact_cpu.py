@@ -126,3 +126,11 @@ def test_workspaces_off_their_alignment():
     lib = specpv.load()
     assert lib.specpv_packed_verify_attn(B(_packed()), B(_tree()), None, None, 0, vp(0x300), None, vp(0x8008), 1 << 40, None) == -1
     assert lib.specpv_evict_tokens(B(_kv()), vp(0x100), 4, 8, 20, B(_kv(k=0x11000, v=0x12000, ctx_len=0x13000)), vp(0x200), vp(0x300), vp(0x8004), 1 << 30, None) == -1
+
+
+def test_rows_of_a_packed_allocation():
+    lib = specpv.load()
+    p = _packed(tokens=-1)
+    assert lib.specpv_packed_workspace_bytes(B(p), B(_tree()), B(_cfg())) == 0
+    assert lib.specpv_pack_tokens(B(_kv()), None, None, None, 4, B(p), None, None, None, None) == -1
+    assert lib.specpv_packed_workspace_bytes(B(_packed(tokens=1000)), B(_tree()), B(_cfg())) == lib.specpv_packed_workspace_bytes(B(_packed()), B(_tree()), B(_cfg())) > 0

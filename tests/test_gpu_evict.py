@@ -115,3 +115,16 @@ def test_binding_refuses(gpu_lib):
     for kw in (dict(dst=src), dict(ws=None), dict(ws=ws[:1000])):
         with pytest.raises(sp.SpecPVError):
             sp.specpv_evict_tokens(src, w, 2, 8, 10, kw.get("dst", dst), idx, None, kw["ws"] if "ws" in kw else ws)
+
+
+def test_memory_that_ends_inside_the_last_block(gpu_lib):
+    """A destination whose blocks would hold the kept tokens, but whose memory does not, is refused."""
+    sp = gpu_lib
+    z = lambda t: torch.zeros((1, 2, t, 64), dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    i1 = lambda: torch.zeros((1,), dtype=torch.int32, device="cuda")  # noqa: E731
+    src = sp.KV(z(64), z(64), i1(), 16)
+    w, idx = torch.zeros((1, 2, 64), device="cuda"), torch.zeros((1, 2, 20), dtype=torch.int32, device="cuda")
+    ws = torch.zeros((sp.specpv_evict_workspace_bytes(src),), dtype=torch.uint8, device="cuda")
+    sp.specpv_evict_tokens(src, w, 2, 8, 10, sp.KV(z(20), z(20), i1(), 16), idx, None, ws)
+    with pytest.raises(ValueError):
+        sp.specpv_evict_tokens(src, w, 2, 8, 10, sp.KV(z(19), z(19), i1(), 16), idx, None, ws)

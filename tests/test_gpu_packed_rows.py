@@ -230,3 +230,18 @@ def test_a_length_beyond_the_source(gpu_lib):
     rows = torch.tensor([[20, 15, 16, 39]], dtype=torch.int32, device="cuda")
     sp.specpv_pack_tokens(src, t.h, src_rows=rows, dst_begin=torch.tensor([30], dtype=torch.int32, device="cuda"))
     _same(t, _expect(want, (k, v), [(0, 31, 15)]))
+
+
+def test_memory_that_ends_inside_the_last_block(gpu_lib):
+    """Rows that max_blocks counts and the allocation does not have are not written."""
+    sp = gpu_lib
+    src, k, v = _source(sp, 1, 2, 60, 64, torch.bfloat16, "bhtd", 9)
+    big = [torch.full((1, 2, 60, w), KEEP, dtype=torch.uint8, device="cuda") for w in (32, 32, 2, 2)]
+    h = sp.PackedKV(*(t[:, :, :40] for t in big), torch.zeros((1,), dtype=torch.int32, device="cuda"), 24, dtype=torch.bfloat16)
+    assert h.max_blocks * h.B == 48
+    kmax, kmin = (torch.zeros(h.summary_shape(), dtype=torch.bfloat16, device="cuda") for _ in "xn")
+    sp.specpv_pack_tokens(src, h, kmax=kmax, kmin=kmin)
+    want = _expect([np.full(t.shape, KEEP, dtype=np.uint8) for t in big], (k, v), [(0, i, i) for i in range(40)])
+    for t, w in zip(big, want):
+        assert np.array_equal(t.cpu().numpy(), w)
+    assert np.array_equal(kmax[0, :, 1].double().cpu().numpy(), k[0, :, 24:40].max(1))
