@@ -196,3 +196,49 @@ def test_two_graphs_in_one_workspace(gpu_lib):
         torch.cuda.synchronize()
         for loop, w in zip(loops, want):
             assert all(torch.equal(a, b) for a, b in zip(loop.outs, w)), i
+
+
+def test_offsets_beyond_32_bits(gpu_lib):
+    """Rows 64 KiB apart, 4.5 GB from first to last: the same bits as from the same rows side by side."""
+    sp = gpu_lib
+    T, L, Dh = 70032, 70021, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = [torch.randn((1, T, 1, Dh), generator=g, device="cuda").bfloat16() for _ in "kv"]
+    i1 = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")  # noqa: E731
+    near = sp.KV(rows[0], rows[1], i1(L), 24, layout="bthd")
+    apart = [torch.empty((1, T, 1, 32768), dtype=torch.bfloat16, device="cuda")[..., :Dh] for _ in "kv"]
+    for a, b in zip(apart, rows):
+        a.copy_(b)
+    far = sp.KV(apart[0], apart[1], i1(L), 24, layout="bthd")
+    q = torch.randn((1, 5, 4, Dh), generator=g, device="cuda").bfloat16()
+    kd, vd = (torch.randn((1, 5, 1, Dh), generator=g, device="cuda").bfloat16() for _ in "kv")
+    tree = sp.Tree(q, kd, vd, torch.arange(-1, 4, dtype=torch.int32, device="cuda")[None])
+    lse = torch.full((1, 5, 4), 12.0, device="cuda")
+    ends = [torch.zeros((1, 1, T), device="cuda") for _ in "ab"]
+    for kv, w in zip((near, far), ends):
+        sp.specpv_accumulate_weights(kv, tree, lse, w)
+    assert torch.equal(*ends) and ends[0][0, 0, L - 1] > 0
+    kept = []
+    for kv, w in zip((near, far), ends):
+        dst = sp.KV(*(torch.zeros((1, 5000, 1, Dh), dtype=torch.bfloat16, device="cuda") for _ in "kv"), i1(0), 20, layout="bthd")
+        idx = torch.zeros((1, 1, 5000), dtype=torch.int32, device="cuda")
+        sp.specpv_evict_tokens(kv, w, 4, 100, 4896, dst, idx, None, torch.zeros((sp.specpv_evict_workspace_bytes(kv),), dtype=torch.uint8, device="cuda"))
+        kept.append((dst.k, dst.v, idx))
+    assert all(torch.equal(a, b) for a, b in zip(*kept)) and int(kept[0][2][0, 0, -1]) == L - 1
+    del far, apart
+    z = lambda wide, w: torch.empty((1, T, 1, wide), dtype=torch.uint8, device="cuda")[..., :w]  # noqa: E731
+    packs = [sp.PackedKV(z(32, 32), z(32, 32), z(2, 2), z(2, 2), i1(L), 24, layout="bthd"),
+             sp.PackedKV(z(65536, 32), z(65536, 32), z(4096, 2), z(4096, 2), i1(L), 24, layout="bthd")]
+    sel, cnt = torch.tensor([[[2917, 0, 5, 2900, 1400, -1]]], dtype=torch.int32, device="cuda"), torch.tensor([[6]], dtype=torch.int32, device="cuda")
+    ws = torch.zeros((sp.specpv_packed_workspace_bytes(packs[0], tree, sp.SelectCfg(0, 0, 6)),), dtype=torch.uint8, device="cuda")
+    got = []
+    for p in packs:
+        sp.specpv_pack_tokens(near, p)
+        o = [torch.zeros((1, 1, 6 * 24, Dh), dtype=torch.bfloat16, device="cuda") for _ in "kv"] + [torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(lse)]
+        sp.specpv_packed_gather_blocks(p, sel, cnt, o[0], o[1])
+        sp.specpv_packed_verify_attn(p, tree, sel, cnt, o[2], None, ws)
+        sp.specpv_packed_verify_attn(p, tree, None, None, o[3], o[4], ws)
+        got.append(o)
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][0].abs().sum() > 0 and torch.isfinite(got[0][4]).all()
+    last = got[0][0][0, 0, :L - 2917 * 24].float()
+    assert (last - rows[0][0, 2917 * 24:L, 0].float()).abs().max() < 1.0       # 4 bits: at most half of the last step, 2^e with e <= 0
