@@ -55,14 +55,14 @@ __device__ __forceinline__ float fold32(const float (&v)[16], int lane)
     return d + __shfl_xor(d, 16);
 }
 
-// A workgroup has WAVES wavefronts (launch_weigh).  A stage's query rows are found and fetched by all of its threads, on their way to
+// A workgroup has WAVES wavefronts, SPLIT of them to each 32 tokens, which share the tiles of query rows between them (launch_weigh).  A stage's query rows are found and fetched by all of its threads, on their way to
 // registers while the stage before is worked on; what rows cost is the less, the more wavefronts they are fetched for.
-template <typename T, int D, int WAVES> struct WeighTile {
+template <typename T, int D, int WAVES, int SPLIT> struct WeighTile {
     static constexpr int E = Elem<T>::kPerVec, STEPS = D / (2 * E);        // channels of a lane's 16 bytes; products of a tile
     static constexpr int PIECES = D / E;                                   // 16-byte pieces of a row
-    static constexpr int MINE = PIECES == 32 ? 4 : 2;                      // pieces of a stage that a thread brings
+    static constexpr int MINE = SPLIT > 1 ? SPLIT * PIECES / (2 * WAVES) : (PIECES == 32 ? 4 : 2);   // pieces of a stage that a thread brings
     static constexpr int ROWS = MINE * 64 * WAVES / PIECES;                // query rows of a stage
-    static_assert(ROWS % 32 == 0, "whole tiles");
+    static_assert(ROWS % (32 * SPLIT) == 0, "whole tiles");
     // so that the 16 lanes that LDS serves at a time find their pieces in different banks
     static __device__ __forceinline__ int place(int row, int piece)
     {
@@ -70,10 +70,10 @@ template <typename T, int D, int WAVES> struct WeighTile {
     }
 };
 
-template <typename T, int D, int WAVES, bool LISTS>
+template <typename T, int D, int WAVES, int SPLIT, bool LISTS>
 __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
 {
-    typedef WeighTile<T, D, WAVES> W;
+    typedef WeighTile<T, D, WAVES, SPLIT> W;
     constexpr int STEPS = W::STEPS, THREADS = 64 * WAVES;
     __shared__ uint4 q_lds[2][W::ROWS * W::PIECES];
     __shared__ float lse_lds[2][W::ROWS];   // -lse * log2 e; -inf: no such row
@@ -86,13 +86,13 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
     const int nb = (int)k.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
     int span = L;   // positions that there are
     if (LISTS) span = max(min(k.a.sel_count[bg], k.a.n_sel), 0) * s.B;
-    const int p0 = (int)blockIdx.x * (WAVES * 32);
+    const int p0 = (int)blockIdx.x * (WAVES / SPLIT * 32);
     if (p0 >= span || L == 0) return;
     // ---- the wavefront's K rows ----
     int tok = -1;
     uint4 kk[STEPS];
     {
-        const int p = p0 + wave * 32 + col;
+        const int p = p0 + wave / SPLIT * 32 + col;
         if (p < span) {
             tok = p;
             if (LISTS) {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
         const int rows = min(W::ROWS, R - r0);
-        for (int t0 = 0; t0 < rows; t0 += 32) {
+        for (int t0 = wave % SPLIT * 32; t0 < rows; t0 += 32 * SPLIT) {
             f32x16 sc;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = 0.f;
@@ -159,7 +159,15 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
         }
     }
     // ---- fold the columns; value i of a tile is its token 8 * (i >> 2) + 4 * half + (i & 3) ----
-    const float w = fold32(sum, lane);
+    float w = fold32(sum, lane);
+    if constexpr (SPLIT > 1) {   // the shares of the wavefronts that have the same tokens, in their order
+        __shared__ float shares[WAVES][64];
+        shares[wave][lane] = w;
+        __syncthreads();
+        if (wave % SPLIT) return;
+#pragma unroll
+        for (int x = 1; x < SPLIT; ++x) w += shares[wave + x][lane];
+    }
     const int i = ((lane & 1) << 3) | ((lane & 2) << 1) | ((lane & 4) >> 1) | ((lane & 8) >> 3);
     const int t = __shfl(tok, 8 * (i >> 2) + 4 * half + (i & 3));
     if ((lane & 16) || t < 0) return;
@@ -182,21 +190,25 @@ hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream
     // 8K 28.3 / 25.4.)  Sixteen for bf16 at 128 channels where every CU gets tokens for those (8 / 16: 128 rows, 8K 8.6 / 10.4, 16K 12.5 / 11.9; 240, 16K
     // 17.3 / 15.9, 32K 30.3 / 29.4; 480, 8K 18.9 / 21.5, 32K 48.9 / 45.1; 64 channels, 240, 64K 35.7 / 36.2; fp32, 64 channels, 128, 32K 46.9 / 47.9): one such
     // workgroup to a CU has nobody to compute while it reads its K rows, but reads each fragment of Q for sixteen.
+    // Four wavefronts to the same 32 tokens from 96 rows on where a CU gets 64 tokens or less: a wavefront by itself would work on while most of the
+    // chip has nothing to do (one to four of eight wavefronts: bf16, 128 channels, 2K, 52 rows 5.1 / 5.5, 112 6.9 / 6.1, 240 10.0 / 7.9, 480 18.4 / 14.4, 4K,
+    // 240 11.3 / 17.2; 64 channels, 2K, 240 7.1 / 5.4; fp32, 128 channels, 2K, 52 11.4 / 11.5, 112 19.1 / 14.1, 240 35.8 / 22.7, 4K, 240 36.0 / 41.8).
     const int64_t each = positions * s.batch * s.Hkv / device_cu_count();   // tokens of a CU
     const bool wide = dtype == SPECPV_BF16 && s.D == 128 && rows >= 128 && each >= 512;
+    const bool few = rows >= 96 && each <= 64;
     const bool many = (rows >= 64 && each >= 256) || (dtype == SPECPV_BF16 && rows >= 192);
-#define SPECPV_WEIGH_L(T, DD, WAVES, LISTS)                                                                              \
+#define SPECPV_WEIGH_L(T, DD, WAVES, SPLIT, LISTS)                                                                              \
     do {                                                                                                                 \
-        const dim3 grid((unsigned)((positions + WAVES * 32 - 1) / (WAVES * 32)), s.Hkv, s.batch);                        \
-        hipLaunchKernelGGL((weigh_kernel<T, DD, WAVES, LISTS>), grid, dim3(64 * WAVES), 0, st, k);                       \
+        const dim3 grid((unsigned)((positions + WAVES / SPLIT * 32 - 1) / (WAVES / SPLIT * 32)), s.Hkv, s.batch);                        \
+        hipLaunchKernelGGL((weigh_kernel<T, DD, WAVES, SPLIT, LISTS>), grid, dim3(64 * WAVES), 0, st, k);                       \
     } while (0)
-#define SPECPV_WEIGH_W(T, DD, WAVES) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, WAVES, true); else SPECPV_WEIGH_L(T, DD, WAVES, false); } while (0)
+#define SPECPV_WEIGH_W(T, DD, WAVES, SPLIT) do { if (a.sel_idx) SPECPV_WEIGH_L(T, DD, WAVES, SPLIT, true); else SPECPV_WEIGH_L(T, DD, WAVES, SPLIT, false); } while (0)
 #define SPECPV_WEIGH(T, DD)                                                                                              \
     do {                                                                                                                 \
         if constexpr (sizeof(T) == 2 && DD == 128) {                                                                     \
-            if (wide) { SPECPV_WEIGH_W(T, DD, 16); break; }                                                              \
+            if (wide) { SPECPV_WEIGH_W(T, DD, 16, 1); break; }                                                              \
         }                                                                                                                \
-        if (many) SPECPV_WEIGH_W(T, DD, 8); else SPECPV_WEIGH_W(T, DD, 4);                                               \
+        if (few) SPECPV_WEIGH_W(T, DD, 8, 4); else if (many) SPECPV_WEIGH_W(T, DD, 8, 1); else SPECPV_WEIGH_W(T, DD, 4, 1);                                               \
     } while (0)
     if (dtype == SPECPV_BF16) {
         if (s.D == 128) SPECPV_WEIGH(bf16_t, 128); else SPECPV_WEIGH(bf16_t, 64);

@@ -135,3 +135,17 @@ def test_many_rows_of_many_tokens(gpu_lib, dtype, D, batch, Hq, M, layout):
     cnt = torch.randint(0, T // 16 + 1, (batch, 2), generator=g).to(torch.int32)
     c.check(gpu_lib, nodes, n.cuda())
     c.check(gpu_lib, idx=idx.cuda(), cnt=cnt.cuda())
+
+
+@pytest.mark.parametrize("dtype,D,Hq,M,lens,layout", [(torch.bfloat16, 128, 6, 33, [700, 0, 33], "bhtd"), (torch.bfloat16, 64, 16, 100, [65], "bthd"), (torch.float32, 128, 8, 64, [321, 32], "bthd"),
+                                                      (torch.float32, 64, 10, 128, [1, 200], "bhtd")])
+def test_many_rows_of_few_tokens(gpu_lib, dtype, D, Hq, M, lens, layout):
+    """Wavefronts that share the rows of the same tokens: whole caches, some rows, lists with blocks twice."""
+    c = Case(gpu_lib, dtype, D, Hq, 2, M, 16, lens, layout, seed=M)
+    c.check(gpu_lib)
+    g = torch.Generator().manual_seed(8)
+    n = torch.tensor([M, M // 2 + 1, 0][:len(lens)], dtype=torch.int32, device="cuda")
+    c.check(gpu_lib, torch.randint(-1, M + 1, (len(lens), M), generator=g).to(torch.int32).cuda(), n)
+    idx = torch.randint(-1, max(lens) // 16 + 2, (len(lens), 2, 7), generator=g).to(torch.int32).cuda()
+    cnt = torch.randint(0, 8, (len(lens), 2), generator=g).to(torch.int32).cuda()
+    c.check(gpu_lib, idx=idx, cnt=cnt)
