@@ -658,9 +658,9 @@ static PackedShape make_packed(const specpv_packed_kv *p, const specpv_tree *tre
 // fp32 ones with them.
 static bool packed_half(const Shape &s, int dtype) { return dtype == SPECPV_BF16 && s.D == 128 && s.koff == 0; }
 static size_t packed_row_bytes(const Shape &s, int dtype) { return (size_t)s.D * (packed_half(s, dtype) ? 2 : 4); }
-static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
+static size_t packed_bytes(const Shape &s, int dtype, int64_t partials)   // (of all rows of a KV head each)
 {
-    const size_t rows = (size_t)s.batch * s.Hq * nsplit * s.M;
+    const size_t rows = (size_t)partials * s.M * s.G;
     return kArriveBytes + align_up(rows * packed_row_bytes(s, dtype)) + align_up(rows * 2 * sizeof(float));
 }
 
@@ -672,8 +672,17 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t nsplit)
 // Where one workgroup to a CU leaves a third of the CUs idle, twice as many, of four wavefronts where there are such (20 sequences of 8K, one token: 38.4 /
 // 34.6; of 4K, 8 tokens: 33.2 / 25.0; 12 of 8K, a quarter idle: 23.2 / 26.2).  No more than a split to four chunks, and 64 (two KV heads, 64K, 32 / 64 / 128:
 // 17.1 / 15.1 / 17.1).
-struct PackedPlan { int64_t ns; int waves; };
-static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks)
+// Whole caches of three sequences and more: one share of all chunks to a CU instead (StreamShare), however long each sequence is, where a share is long against
+// what each pair in it costs, taking the batch for one of lengths 1 : 2 : 3 : ..., whose shortest come several to a share.  (us, splits / shares,
+// lengths 1 : 2 : ... and equal, 8 KV heads: 60 query tokens, 8 x 32K 281 / 209 and 321 / 322; 73, 3 x 35K 155 / 130 and 165 / 181; one, 8 x 32K 40.6 / 33.4
+// and 49.6 / 50.8, 4 x 128K 73.5 / 61.8 and 92.3 / 91.3; fp32, 30, 6 x 9K 102 / 74 and 112 / 89; not so 16 tokens, 16 x 16K 78 / 87 and 95 / 96; one, 16 x 8K
+// 23.2 / 27.7 and 28.5 / 29.4; two sequences of 72K, 21 tokens 69.8 / 65.3 and 75.4 / 82.8.)
+struct PackedPlan {
+    int64_t ns, stream;   // splits of every pair, or (stream > 0) shares of all
+    int waves;
+    int64_t partials(const Shape &s) const { const int64_t pairs = (int64_t)s.batch * s.Hkv; return stream ? stream + pairs : ns * pairs; }
+};
+static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks, bool lists)
 {
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
     const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype), cus = device_cu_count();
@@ -683,7 +692,9 @@ static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks)
     if (idle) ns = 2 * cus / columns;
     if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
     if (ns > 64) ns = 64;
-    return {ns < 1 ? 1 : ns, waves};
+    const int64_t stream = cus / packed_row_tiles(s, dtype), behind = (int64_t)s.batch * (s.batch + 1) / 2 * s.Hkv;
+    if (!lists && s.batch >= 3 && s.batch <= 64 && stream > 0 && packed_runs(s, false) && chunks * s.batch * s.Hkv >= 64 * (stream + behind)) return {1, stream, 8};
+    return {ns < 1 ? 1 : ns, 0, waves};
 }
 
 }  // namespace specpv
@@ -964,10 +975,10 @@ size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tr
     if (!tree) return kArriveBytes + 256;
     if (check_tree(&plain, tree, false) != SPECPV_OK) return 0;
     const Shape s = make_shape(&plain, tree);
-    size_t need = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, s.max_blocks).ns);
+    size_t need = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, s.max_blocks, false).partials(s));
     if (cfg) {
         const int64_t n_sel = (int64_t)cfg->n_sink_blocks + cfg->k_blocks + cfg->n_recent_blocks + cfg->n_extra_slots;
-        const size_t lists = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, n_sel).ns), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
+        const size_t lists = packed_bytes(s, kv->dtype, packed_plan(s, kv->dtype, n_sel, true).partials(s)), scores = kArriveBytes + align_up((size_t)s.batch * s.Hkv * s.max_blocks * sizeof(float));
         if (lists > need) need = lists;
         if (scores > need) need = scores;
     }
@@ -999,14 +1010,14 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     const PackedShape p = make_packed(kv, tree);
     const Shape &s = p.s;
     if ((uintptr_t)workspace & 15) return SPECPV_EINVAL;
-    if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, 1)) return SPECPV_EWORKSPACE;
-    const PackedPlan plan = packed_plan(s, kv->dtype, sel_idx ? n_sel : s.max_blocks);
-    int64_t ns = plan.ns;
-    while (ns > 1 && packed_bytes(s, kv->dtype, ns) > workspace_bytes) --ns;
-    if ((int64_t)packed_row_tiles(s, kv->dtype) * ns > 65535) return SPECPV_ELIMIT;
-    const size_t rows = (size_t)s.batch * s.Hq * ns * s.M;
+    const int64_t pairs = (int64_t)s.batch * s.Hkv;
+    if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, pairs)) return SPECPV_EWORKSPACE;
+    PackedPlan plan = packed_plan(s, kv->dtype, sel_idx ? n_sel : s.max_blocks, sel_idx != nullptr);
+    while (plan.partials(s) > pairs && packed_bytes(s, kv->dtype, plan.partials(s)) > workspace_bytes) --(plan.stream ? plan.stream : plan.ns);
+    if ((int64_t)packed_row_tiles(s, kv->dtype) * plan.ns > 65535) return SPECPV_ELIMIT;
+    const size_t rows = (size_t)plan.partials(s) * s.M * s.G;
     char *const at = (char *)workspace + kArriveBytes;
-    const Partials part{(float *)at, (float *)(at + align_up(rows * packed_row_bytes(s, kv->dtype))), (int)ns, packed_half(s, kv->dtype) ? 1 : 0, 0, nullptr};
+    const Partials part{(float *)at, (float *)(at + align_up(rows * packed_row_bytes(s, kv->dtype))), (int)plan.ns, packed_half(s, kv->dtype) ? 1 : 0, (int)plan.stream, nullptr};
     hipError_t e = launch_packed_attn(p, kv->dtype, sel_idx, sel_count, n_sel, part, plan.waves, (hipStream_t)stream);
     if (e == hipSuccess) e = launch_combine(s, kv->dtype, part, out, lse, (hipStream_t)stream);
     return e == hipSuccess ? SPECPV_OK : fail_hip(e);

@@ -82,7 +82,8 @@ template <int D> struct RowTile<16, D> {
     static __device__ __forceinline__ float col_sum(float x) { return sum_xor32(xor16(x, true)); }
 };
 
-template <typename T, int D, int RT, bool RUN, int WAVES>
+// SHARES: workgroup w has the chunks that are its share of all (sequence, KV head) pairs' (StreamShare), of one pair or of several.
+template <typename T, int D, int RT, bool RUN, int WAVES, bool SHARES>
 __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnArgs a)
 {
     typedef RowTile<RT, D> Tile;
@@ -100,17 +101,47 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
     const Shape &s = a.p.s;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & (RT - 1), part = lane / RT;
-    const int bg = blockIdx.x, b = (int)a.div_hkv.div((uint32_t)bg), g = bg - b * s.Hkv;
-    const int split = (int)a.div_tiles.div(blockIdx.y), tile = (int)blockIdx.y - split * a.row_tiles;
-    const int R = s.M * s.G, r = tile * RT + col;
-    const bool row_live = r < R;
     const int64_t cap = (int64_t)s.max_blocks * s.B;
+    const int R = s.M * s.G;
+    int x = 0, x1 = 0, seq_chunks = 0, seq_upto = 0;   // SHARES: chunks from here to there, in the row of all pairs' (and see StreamShare)
+    if constexpr (SHARES) {
+        const StreamShare sh(s, lane, a.part.stream);
+        if ((int)blockIdx.x >= sh.wgs) return;
+        x = sh.begin((int)blockIdx.x);
+        x1 = sh.begin((int)blockIdx.x + 1);
+        seq_chunks = sh.chunks;
+        seq_upto = sh.upto;
+    }
+    do {
+    int bg = blockIdx.x, b, g, tile = blockIdx.y, c0, c1;
+    int64_t slot;
+    if constexpr (SHARES) {
+        b = __builtin_ctzll(__ballot(lane < s.batch && seq_upto * s.Hkv > x));
+        const int C = __builtin_amdgcn_readlane(seq_chunks, b), from = x - (__builtin_amdgcn_readlane(seq_upto, b) - C) * s.Hkv;
+        g = (int)((uint32_t)from / (uint32_t)C);
+        c0 = from - g * C;
+        c1 = min(C, c0 + x1 - x);
+        bg = b * s.Hkv + g;
+        slot = (int64_t)blockIdx.x + bg;
+    } else {
+        b = (int)a.div_hkv.div((uint32_t)bg);
+        g = bg - b * s.Hkv;
+        const int split = (int)a.div_tiles.div(blockIdx.y);
+        tile -= split * a.row_tiles;
+        slot = (int64_t)bg * a.part.nsplit + split;
+        c0 = split;   // (and see below)
+    }
+    const int r = tile * RT + col;
+    const bool row_live = r < R;
     const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
     const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
     int span = L;
     if (a.sel_idx) span = L ? max(min(a.sel_count[bg], a.n_sel), 0) * s.B : 0;
-    const int chunks = (int)(((uint32_t)span + 31u) >> 5);
-    const int c0 = (int)((int64_t)chunks * split / a.part.nsplit), c1 = (int)((int64_t)chunks * (split + 1) / a.part.nsplit);
+    if constexpr (!SHARES) {
+        const int chunks = (int)(((uint32_t)span + 31u) >> 5);
+        c1 = (int)((int64_t)chunks * (c0 + 1) / a.part.nsplit);
+        c0 = (int)((int64_t)chunks * c0 / a.part.nsplit);
+    }
 
     // ---- query rows: the B operand of step i is channels part * SHARE + 8 i .. + 7 ----
     bf16x8 q[N][STEPS];
@@ -373,24 +404,31 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
         wt[x] = __builtin_amdgcn_exp2f(o.x - ref);
         l = fmaf(o.y, wt[x], l);
     }
-    if (!row_live) return;
-    const int64_t prow = ((int64_t)bg * a.part.nsplit + split) * R + r;
-    // (the combine kernel takes a partial by l > 0: a sum that is no number is handed on in the maximum's place)
-    if (wave == 0 && part == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
-    const float inv = l != 0.f ? 1.f / l : 0.f;
+    if (row_live) {
+        const int64_t prow = slot * R + r;
+        // (the combine kernel takes a partial by l > 0: a sum that is no number is handed on in the maximum's place)
+        if (wave == 0 && part == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
+        const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int i = 0; i < (VALUES / 4 + WAVES - 1) / WAVES; ++i) {
-        const int at = i * WAVES + wave;
-        if (at >= VALUES / 4) break;
-        float o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < (VALUES / 4 + WAVES - 1) / WAVES; ++i) {
+            const int at = i * WAVES + wave;
+            if (at >= VALUES / 4) break;
+            float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int x = 0; x < WAVES; ++x) {
-            const float4 v = ((const float4 *)lds[x])[at * 64 + lane];
-            o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
+            for (int x = 0; x < WAVES; ++x) {
+                const float4 v = ((const float4 *)lds[x])[at * 64 + lane];
+                o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
+            }
+            const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
+            store_partial(a.part, prow, ch, D, o, inv);
         }
-        const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
-        store_partial(a.part, prow, ch, D, o, inv);
     }
+    if constexpr (SHARES) {
+        x += c1 - c0;
+        if (x >= x1) break;
+        __syncthreads();   // (the results' places are wanted again)
+    }
+    } while (SHARES);
 }
 
 hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *sel_idx, const int32_t *sel_count, int n_sel, Partials part,
@@ -401,15 +439,23 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     const int rt = packed_row_tile(s, dtype), tiles = packed_row_tiles(s, dtype);
     const PackedAttnArgs a{p, part, sel_idx, sel_count, n_sel, tiles, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.Hkv),
                            make_fastdiv((uint32_t)s.M), make_fastdiv((uint32_t)tiles), kLog2e / sqrtf((float)s.D)};
-    const dim3 grid(s.batch * s.Hkv, tiles * part.nsplit);
-#define SPECPV_ATTN_W(T, DD, R, RUN, WAVES) hipLaunchKernelGGL((packed_attn_kernel<T, DD, R, RUN, WAVES>), grid, dim3(64 * WAVES), 0, st, a)
-#define SPECPV_ATTN_R(T, DD, RUN)                                                                                                       \
-    do {                                                                                                                                \
-        if (rt == 16) {                                                                                                                 \
-            if (sizeof(T) == 2 || waves == 8) SPECPV_ATTN_W(T, DD, 16, RUN, 8); else if constexpr (sizeof(T) == 4) SPECPV_ATTN_W(T, DD, 16, RUN, 4); \
-        } else if constexpr (sizeof(T) == 2 || DD == 64) {                                                                              \
-            if (waves == 8) SPECPV_ATTN_W(T, DD, 32, RUN, 8); else SPECPV_ATTN_W(T, DD, 32, RUN, 4);                                    \
-        }                                                                                                                               \
+    const dim3 grid(part.stream ? part.stream : s.batch * s.Hkv, tiles * (part.stream ? 1 : part.nsplit));
+#define SPECPV_ATTN_W(T, DD, R, RUN, WAVES, SHARES) \
+    hipLaunchKernelGGL((packed_attn_kernel<T, DD, R, RUN, WAVES, SHARES>), grid, dim3(64 * WAVES), 0, st, a)
+#define SPECPV_ATTN_S(T, DD, R, RUN)                                                                     \
+    do {                                                                                                 \
+        if constexpr (RUN) {                                                                             \
+            if (part.stream) { SPECPV_ATTN_W(T, DD, R, true, 8, true); break; }                          \
+        }                                                                                                \
+        if constexpr (sizeof(T) == 4 || R == 32) {                                                       \
+            if (waves == 4) { SPECPV_ATTN_W(T, DD, R, RUN, 4, false); break; }                           \
+        }                                                                                                \
+        SPECPV_ATTN_W(T, DD, R, RUN, 8, false);                                                          \
+    } while (0)
+#define SPECPV_ATTN_R(T, DD, RUN)                                                                        \
+    do {                                                                                                 \
+        if (rt == 16) SPECPV_ATTN_S(T, DD, 16, RUN);                                                     \
+        else if constexpr (sizeof(T) == 2 || DD == 64) SPECPV_ATTN_S(T, DD, 32, RUN);                    \
     } while (0)
 #define SPECPV_ATTN(T, DD) do { if (run) SPECPV_ATTN_R(T, DD, true); else SPECPV_ATTN_R(T, DD, false); } while (0)
     if (dtype == SPECPV_BF16) {
@@ -419,6 +465,7 @@ hipError_t launch_packed_attn(const PackedShape &p, int dtype, const int32_t *se
     }
 #undef SPECPV_ATTN
 #undef SPECPV_ATTN_R
+#undef SPECPV_ATTN_S
 #undef SPECPV_ATTN_W
     return hipGetLastError();
 }

@@ -170,3 +170,25 @@ def test_splits_of_every_kind(gpu_lib, dtype, D, M, Hq, Hkv, lens):
     h, k, v = ref.cache(sp, len(lens), Hkv, T, D, 64, dtype, seed=M, lens=lens)
     tree, tv, parent = _tree(sp, len(lens), M, 0, Hq, Hkv, D, dtype, M + D)
     check(sp, h, (k, v), tree, tv, parent)
+
+
+@pytest.mark.parametrize("dtype,D,M,Hq,Hkv,lens,Bk", [(torch.bfloat16, 128, 2, 4, 2, [91600, 0, 40000], 64), (torch.bfloat16, 64, 128, 16, 1, [5701, 33, 0, 64, 700], 24),
+                                                      (torch.bfloat16, 128, 60, 10, 2, [1, 9000, 4000, 8999], 64), (torch.float32, 64, 60, 10, 2, [9000, 1, 33], 40),
+                                                      (torch.float32, 128, 40, 4, 1, [9000, 20, 5120], 64), (torch.bfloat16, 64, 1, 4, 2, [0, 0, 91600], 16),
+                                                      (torch.bfloat16, 64, 128, 16, 1, [7999, 33, 0, 64, 700], 24), (torch.bfloat16, 128, 60, 10, 2, [1, 12000, 4000, 8999], 64),
+                                                      (torch.float32, 64, 60, 10, 2, [13000, 1, 33], 40), (torch.float32, 128, 40, 4, 1, [21500, 20, 5120], 64)])
+def test_shares_of_batches(gpu_lib, dtype, D, M, Hq, Hkv, lens, Bk):
+    """Long whole caches of three sequences and more, some of them empty or nearly so; in less workspace; and none left at all."""
+    sp = gpu_lib
+    T = -(-max(lens) // Bk) * Bk
+    h, k, v = ref.cache(sp, len(lens), Hkv, T, D, Bk, dtype, "bthd" if M == 60 else "bhtd", seed=M, lens=lens)
+    tree, tv, parent = _tree(sp, len(lens), M, 0, Hq, Hkv, D, dtype, M + D)
+    check(sp, h, (k, v), tree, tv, parent)
+    full = sp.specpv_packed_workspace_bytes(h, tree)
+    rows = len(lens) * Hq * M          # results of one split and their sums, each in whole 256 bytes
+    one = 65536 + sum(-(-x // 256) * 256 for x in (rows * D * (2 if dtype == torch.bfloat16 and D == 128 else 4), rows * 8))
+    assert one <= full
+    for size in (one, one + (full - one) // 3):
+        check(sp, h, (k, v), tree, tv, parent, ws=torch.zeros((size,), dtype=torch.uint8, device="cuda"))
+    h.ctx_len.zero_()
+    check(sp, h, (k, v), tree, tv, parent)
