@@ -112,322 +112,321 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
         seq_chunks = sh.chunks;
         seq_upto = sh.upto;
     }
-    do {
-    int bg = blockIdx.x, b, g, tile = blockIdx.y, c0, c1;
-    int64_t slot;
-    if constexpr (SHARES) {
-        b = __builtin_ctzll(__ballot(lane < s.batch && seq_upto * s.Hkv > x));
-        const int C = __builtin_amdgcn_readlane(seq_chunks, b), from = x - (__builtin_amdgcn_readlane(seq_upto, b) - C) * s.Hkv;
-        g = (int)((uint32_t)from / (uint32_t)C);
-        c0 = from - g * C;
-        c1 = min(C, c0 + x1 - x);
-        bg = b * s.Hkv + g;
-        slot = (int64_t)blockIdx.x + bg;
-    } else {
-        b = (int)a.div_hkv.div((uint32_t)bg);
-        g = bg - b * s.Hkv;
-        const int split = (int)a.div_tiles.div(blockIdx.y);
-        tile -= split * a.row_tiles;
-        slot = (int64_t)bg * a.part.nsplit + split;
-        c0 = split;   // (and see below)
-    }
-    const int r = tile * RT + col;
-    const bool row_live = r < R;
-    const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
-    const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
-    int span = L;
-    if (a.sel_idx) span = L ? max(min(a.sel_count[bg], a.n_sel), 0) * s.B : 0;
-    if constexpr (!SHARES) {
-        const int chunks = (int)(((uint32_t)span + 31u) >> 5);
-        c1 = (int)((int64_t)chunks * (c0 + 1) / a.part.nsplit);
-        c0 = (int)((int64_t)chunks * c0 / a.part.nsplit);
-    }
-
-    // ---- query rows: the B operand of step i is channels part * SHARE + 8 i .. + 7 ----
-    bf16x8 q[N][STEPS];
-    {
-        const int rr = min(r, R - 1), hh = (int)a.div_M.div((uint32_t)rr), j = rr - hh * s.M;
-        const T *row = (const T *)s.q + (((int64_t)b * s.M + j) * s.Hq + (int64_t)g * s.G + hh) * D + part * SHARE;
-#pragma unroll
-        for (int i = 0; i < STEPS; ++i) {
-            if constexpr (N == 1) {
-                q[0][i] = __builtin_bit_cast(bf16x8, *(const uint4 *)(row + 8 * i));
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float f = row[8 * i + e];
-#pragma unroll
-                    for (int n = 0; n < N; ++n) { q[n][i][e] = (__bf16)f; f -= (float)q[n][i][e]; }
-                }
-            }
-        }
-    }
-
-    // ---- where this lane's V loads come from and go to ----
-    // D = 128: lanes 4 u .. 4 u + 3 a token's four groups, 16 lanes tokens 0, 4, 8, 12 (+ lane / 16, + 16 x); D = 64: two
-    // groups, 16 lanes 8 tokens in a row.  In LDS a row's 64-byte units and their 16-byte pieces are permuted by the token, so that
-    // the 16 lanes of a write cover all banks, and so do the rows that half a wavefront's transposing read takes (RT = 32: four of
-    // 64 bytes, RT = 16: eight of 32).
-    auto v_token = [&](int x) { return D == 128 ? 4 * ((lane >> 2) & 3) + (lane >> 4) + 16 * x : lane >> 1; };
-    auto v_place = [&](int t, int unit, int piece) {   // byte of a 16-byte piece
-        const int u = t >> 2 & 3;
-        return D == 128 ? t * VROW + ((unit ^ (t & 3)) << 6) + ((piece ^ ((u & 1) << 1 | u >> 1)) << 4)
-                        : t * VROW + ((unit ^ ((t >> 1) & 1)) << 6) + ((piece ^ ((t >> 1) & 3)) << 4);
-    };
-    const int v_group = lane & (GROUPS - 1);
-    char *const mine = lds[wave];
-
-    const int64_t base = (int64_t)b * s.sb + (int64_t)g * s.sh;
-    const uint8_t *const kc = (const uint8_t *)s.k + base, *const vc = (const uint8_t *)s.v + base;
-    const uint8_t *const ksc = a.p.ks + (base >> 4), *const vsc = a.p.vs + (base >> 4);
-    const int32_t *const list = a.sel_idx ? a.sel_idx + (int64_t)bg * a.n_sel : nullptr;
-    const uint32_t k_lane = (uint32_t)part * (SHARE / 2), v_lane = (uint32_t)v_group * 16, ks_lane = (uint32_t)(part * SHARE) / 32, vs_lane = (uint32_t)v_group;
-
-    typedef ChunkTokens<RUN> Tokens;
-    auto tokens_of = [&](int c) {   // of chunk c < c1 (behind it: of the last one once more)
-        Tokens x;
-        c = min(c, c1 - 1);
-        if constexpr (RUN) {
-            x.row = 32 * c;
-            if (list) {
-                const int slot = (int)a.div_B.div((uint32_t)(32 * c)), e = list[slot];
-                x.row = e >= 0 && e < nb ? e * s.B + (32 * c - slot * s.B) : -1;
-            }
+    do {   // (SHARES: pair by pair)
+        int bg = blockIdx.x, b, g, tile = blockIdx.y, split = 0, c0, c1;
+        int64_t slot;
+        if constexpr (SHARES) {
+            b = __builtin_ctzll(__ballot(lane < s.batch && seq_upto * s.Hkv > x));
+            const int C = __builtin_amdgcn_readlane(seq_chunks, b), from = x - (__builtin_amdgcn_readlane(seq_upto, b) - C) * s.Hkv;
+            g = (int)((uint32_t)from / (uint32_t)C);
+            c0 = from - g * C;
+            c1 = min(C, c0 + x1 - x);
+            bg = b * s.Hkv + g;
+            slot = (int64_t)blockIdx.x + bg;
         } else {
-            const int p = 32 * c + (lane & 31);
-            x.tok = -1;
-            if (p < span) {
-                x.tok = p;
-                if (list) {
-                    const int slot = (int)a.div_B.div((uint32_t)p), e = list[slot];
-                    x.tok = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
-                }
-            }
+            b = (int)a.div_hkv.div((uint32_t)bg);
+            g = bg - b * s.Hkv;
+            split = (int)a.div_tiles.div(blockIdx.y);
+            tile -= split * a.row_tiles;
+            slot = (int64_t)bg * a.part.nsplit + split;
         }
-        return x;
-    };
-    struct Codes {
-        uint32_t k[KT][KWORDS], ks[KT];
-        uint4 v[VLOADS];
-        uint32_t vs[VLOADS];
-        uint32_t live;       // bit t: token t of the chunk counts
-    };
-    auto k_words = [&](const uint8_t *p, uint32_t (&w)[KWORDS]) __attribute__((always_inline)) {
-        if constexpr (KWORDS == 2) {
-            const u32x2 u = load_codes<STREAM>((const u32x2 *)p);
-            w[0] = u[0]; w[1] = u[1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < KWORDS; i += 4) {
-                const u32x4 u = load_codes<STREAM>((const u32x4 *)(p + 4 * i));
-                w[i] = u[0]; w[i + 1] = u[1]; w[i + 2] = u[2]; w[i + 3] = u[3];
-            }
+        const int r = tile * RT + col;
+        const bool row_live = r < R;
+        const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
+        const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
+        int span = L;
+        if (a.sel_idx) span = L ? max(min(a.sel_count[bg], a.n_sel), 0) * s.B : 0;
+        if constexpr (!SHARES) {
+            const int chunks = (int)(((uint32_t)span + 31u) >> 5);
+            c0 = (int)((int64_t)chunks * split / a.part.nsplit);
+            c1 = (int)((int64_t)chunks * (split + 1) / a.part.nsplit);
         }
-    };
-    auto k_scale = [&](const uint8_t *p) __attribute__((always_inline)) { return SHARE == 64 ? (uint32_t) * (const uint16_t *)p : (uint32_t)*p; };
-    // Tokens that are not there are read as another of the chunk, which is; a chunk of none as token 0, and is then left out.
-    auto fetch = [&](const Tokens &tk, Codes &x) __attribute__((always_inline)) {
-        if constexpr (RUN) {
-            const int n = tk.row < 0 ? 0 : min(max(L - tk.row, 0), 32);
-            x.live = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
-            const int row = n > 0 ? tk.row : 0, last = n > 0 ? n - 1 : 0;
-            const int64_t at = (int64_t)row * s.st;
-            const uint8_t *const k0 = kc + at, *const v0 = vc + at, *const ks0 = ksc + (at >> 4), *const vs0 = vsc + (at >> 4);
-            const uint32_t st = (uint32_t)s.st;   // (32 rows lie within 2^31 bytes: launch_packed_attn)
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const uint32_t ko = (uint32_t)min(col + RT * kt, last) * st;
-                k_words(k0 + (ko + k_lane), x.k[kt]);
-                x.ks[kt] = k_scale(ks0 + ((ko >> 4) + ks_lane));
-            }
-#pragma unroll
-            for (int i = 0; i < VLOADS; ++i) {
-                const uint32_t vo = (uint32_t)min(v_token(i), last) * st;
-                x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(v0 + (vo + v_lane))));
-                x.vs[i] = vs0[(vo >> 4) + vs_lane];
-            }
-        } else {
-            const bool there = tk.tok >= 0 && tk.tok < L;
-            const unsigned long long who = __ballot(there);
-            x.live = (uint32_t)who;
-            const int tok = there ? tk.tok : (who ? __builtin_amdgcn_readlane(tk.tok, __builtin_ctzll(who)) : 0);
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const int64_t o = (int64_t)(KT == 1 ? tok : __shfl(tok, col + RT * kt)) * s.st;
-                k_words(kc + o + k_lane, x.k[kt]);
-                x.ks[kt] = k_scale(ksc + (o >> 4) + ks_lane);
-            }
-#pragma unroll
-            for (int i = 0; i < VLOADS; ++i) {
-                const int64_t vo = (int64_t)__shfl(tok, v_token(i)) * s.st;
-                x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(vc + vo + v_lane)));
-                x.vs[i] = vsc[(vo >> 4) + vs_lane];
-            }
-        }
-    };
 
-    Acc O[OT];
-#pragma unroll
-    for (int j = 0; j < OT; ++j)
-#pragma unroll
-        for (int i = 0; i < REGS; ++i) O[j][i] = 0.f;
-    float neg_ref = 3e38f, sum_l = 0.f;   // minus the reference maximum, in log2 units; the lane's sum
-
-    // the lane's addresses for the transposing reads: its token of the four that 16 lanes turn, its 4 channels of tile j
-    uint32_t v_at[2][OT];
-    {
-        const int sl = lane & 15;
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int j = 0; j < OT; ++j) {
-                const int t = (RT == 32 ? 8 : 16) * hf + 4 * part + (sl >> 2);
-                const int byte = 2 * RT * j + (RT == 32 ? 32 * ((lane >> 4) & 1) : 0) + 8 * (sl & 3);   // of the row
-                v_at[hf][j] = (uint32_t)(v_place(t, byte >> 6, (byte >> 4) & 3) + (byte & 15));
-            }
-    }
-    typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
-
-    auto work = [&](const Codes &x) __attribute__((always_inline)) {
-        if (x.live == 0) return;
-        // V as bf16 into LDS
-#pragma unroll
-        for (int i = 0; i < VLOADS; ++i) {
-            const int t = v_token(i);
-            const float sc = scale_of(x.vs[i]);
-            const uint32_t w[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) *(uint4 *)(mine + v_place(t, v_group, e)) = decode8_bf16(w[e], sc);
-        }
-        Acc S[KT];
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-#pragma unroll
-            for (int i = 0; i < REGS; ++i) S[kt][i] = 0.f;
+        // ---- query rows: the B operand of step i is channels part * SHARE + 8 i .. + 7 ----
+        bf16x8 q[N][STEPS];
+        {
+            const int rr = min(r, R - 1), hh = (int)a.div_M.div((uint32_t)rr), j = rr - hh * s.M;
+            const T *row = (const T *)s.q + (((int64_t)b * s.M + j) * s.Hq + (int64_t)g * s.G + hh) * D + part * SHARE;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) {
-                const float sc = scale_of(SHARE == 64 ? (i >> 2 ? x.ks[kt] >> 8 : x.ks[kt] & 0xffu) : x.ks[kt]);
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, decode8_bf16(x.k[kt][i], sc));
+                if constexpr (N == 1) {
+                    q[0][i] = __builtin_bit_cast(bf16x8, *(const uint4 *)(row + 8 * i));
+                } else {
 #pragma unroll
-                for (int n = 0; n < N; ++n) S[kt] = Tile::mfma(kf, q[n][i], S[kt]);
+                    for (int e = 0; e < 8; ++e) {
+                        float f = row[8 * i + e];
+#pragma unroll
+                        for (int n = 0; n < N; ++n) { q[n][i][e] = (__bf16)f; f -= (float)q[n][i][e]; }
+                    }
+                }
             }
         }
-        if (x.live != 0xffffffffu) {
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int i = 0; i < REGS; ++i) S[kt][i] = x.live >> Tile::token(kt, i, part) & 1u ? S[kt][i] : -INFINITY;
-        }
-        // The reference maximum moves where the weights say that it has been left behind: one above 2^12 makes its lane's sum larger
-        // than that (so does the first chunk's, by a reference of -3e38, and one that is no number).  No maximum is looked for elsewhere.
-        float w[KT * REGS], sum;
-        auto weigh = [&]() __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < KT * REGS; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(S[i / REGS][i % REGS], a.scale_log2, neg_ref));
-            // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
-            float t[4] = {w[0], w[1], w[2], w[3]};
-#pragma unroll
-            for (int i = 4; i < KT * REGS; ++i) t[i & 3] += w[i];
-            sum = (t[0] + t[1]) + (t[2] + t[3]);
-        };
-        weigh();
-        if (__any(!(sum <= 4096.f))) {
-            float top = S[0][0];
-#pragma unroll
-            for (int i = 1; i < KT * REGS; ++i) top = fmaxf(top, S[i / REGS][i % REGS]);
-            const float z = Tile::col_max(top) * a.scale_log2, ref = -neg_ref, ref_new = z > ref ? z : ref;
-            const float alpha = __builtin_amdgcn_exp2f(ref - ref_new);
-            neg_ref = -ref_new;
-            sum_l *= alpha;
-#pragma unroll
-            for (int j = 0; j < OT; ++j)
-#pragma unroll
-                for (int i = 0; i < REGS; ++i) O[j][i] *= alpha;
-            weigh();
-        }
-        sum_l += sum;
-#pragma unroll
-        for (int ks = 0; ks < Tile::VSTEPS; ++ks) {
-            bf16x8 pf[N];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float f = w[8 * ks + e];
-#pragma unroll
-                for (int n = 0; n < N; ++n) { pf[n][e] = (__bf16)f; f -= (float)pf[n][e]; }
-            }
-#pragma unroll
-            for (int j = 0; j < OT; ++j) {
-                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[0][j] + ks * 16 * VROW));
-                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[1][j] + ks * 16 * VROW));
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-                for (int n = 0; n < N; ++n) O[j] = Tile::mfma(vf, pf[n], O[j]);
-            }
-        }
-    };
 
-    if (c0 + wave < c1) {
-        Codes even, odd;   // (in turn, so that no registers move)
-        int c = c0 + wave;
-        fetch(tokens_of(c), even);
-        Tokens next = tokens_of(c + WAVES);
-        for (;;) {
-            fetch(next, odd);
-            next = tokens_of(c + 2 * WAVES);
-            work(even);
-            if ((c += WAVES) >= c1) break;
-            fetch(next, even);
-            next = tokens_of(c + 2 * WAVES);
-            work(odd);
-            if ((c += WAVES) >= c1) break;
-        }
-    }
-    // ---- the wavefronts' results into one: all of them to LDS, and each wavefront merges and stores every so-manieth four channels ----
-    float l = Tile::col_sum(sum_l), m = l != 0.f ? -neg_ref : -INFINITY;   // (l may be NaN)
-    ml_lds[wave][lane] = make_float2(m, l);
-    float4 *const own = (float4 *)lds[wave];     // [VALUES / 4][64]
-#pragma unroll
-    for (int i = 0; i < VALUES / 4; ++i) {
-        const Acc &o = O[4 * i / REGS];
-        own[i * 64 + lane] = make_float4(o[4 * i % REGS], o[4 * i % REGS + 1], o[4 * i % REGS + 2], o[4 * i % REGS + 3]);
-    }
-    __syncthreads();
-    float wt[WAVES];
-    m = -INFINITY;
-#pragma unroll
-    for (int x = 0; x < WAVES; ++x) m = fmaxf(m, ml_lds[x][lane].x);
-    const float ref = m == -INFINITY ? 0.f : m;
-    l = 0.f;
-#pragma unroll
-    for (int x = 0; x < WAVES; ++x) {
-        const float2 o = ml_lds[x][lane];
-        wt[x] = __builtin_amdgcn_exp2f(o.x - ref);
-        l = fmaf(o.y, wt[x], l);
-    }
-    if (row_live) {
-        const int64_t prow = slot * R + r;
-        // (the combine kernel takes a partial by l > 0: a sum that is no number is handed on in the maximum's place)
-        if (wave == 0 && part == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-        for (int i = 0; i < (VALUES / 4 + WAVES - 1) / WAVES; ++i) {
-            const int at = i * WAVES + wave;
-            if (at >= VALUES / 4) break;
-            float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < WAVES; ++x) {
-                const float4 v = ((const float4 *)lds[x])[at * 64 + lane];
-                o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
+        // ---- where this lane's V loads come from and go to ----
+        // D = 128: lanes 4 u .. 4 u + 3 a token's four groups, 16 lanes tokens 0, 4, 8, 12 (+ lane / 16, + 16 x); D = 64: two
+        // groups, 16 lanes 8 tokens in a row.  In LDS a row's 64-byte units and their 16-byte pieces are permuted by the token, so that
+        // the 16 lanes of a write cover all banks, and so do the rows that half a wavefront's transposing read takes (RT = 32: four of
+        // 64 bytes, RT = 16: eight of 32).
+        auto v_token = [&](int x) { return D == 128 ? 4 * ((lane >> 2) & 3) + (lane >> 4) + 16 * x : lane >> 1; };
+        auto v_place = [&](int t, int unit, int piece) {   // byte of a 16-byte piece
+            const int u = t >> 2 & 3;
+            return D == 128 ? t * VROW + ((unit ^ (t & 3)) << 6) + ((piece ^ ((u & 1) << 1 | u >> 1)) << 4)
+                            : t * VROW + ((unit ^ ((t >> 1) & 1)) << 6) + ((piece ^ ((t >> 1) & 3)) << 4);
+        };
+        const int v_group = lane & (GROUPS - 1);
+        char *const mine = lds[wave];
+
+        const int64_t base = (int64_t)b * s.sb + (int64_t)g * s.sh;
+        const uint8_t *const kc = (const uint8_t *)s.k + base, *const vc = (const uint8_t *)s.v + base;
+        const uint8_t *const ksc = a.p.ks + (base >> 4), *const vsc = a.p.vs + (base >> 4);
+        const int32_t *const list = a.sel_idx ? a.sel_idx + (int64_t)bg * a.n_sel : nullptr;
+        const uint32_t k_lane = (uint32_t)part * (SHARE / 2), v_lane = (uint32_t)v_group * 16, ks_lane = (uint32_t)(part * SHARE) / 32, vs_lane = (uint32_t)v_group;
+
+        typedef ChunkTokens<RUN> Tokens;
+        auto tokens_of = [&](int c) {   // of chunk c < c1 (behind it: of the last one once more)
+            Tokens x;
+            c = min(c, c1 - 1);
+            if constexpr (RUN) {
+                x.row = 32 * c;
+                if (list) {
+                    const int slot = (int)a.div_B.div((uint32_t)(32 * c)), e = list[slot];
+                    x.row = e >= 0 && e < nb ? e * s.B + (32 * c - slot * s.B) : -1;
+                }
+            } else {
+                const int p = 32 * c + (lane & 31);
+                x.tok = -1;
+                if (p < span) {
+                    x.tok = p;
+                    if (list) {
+                        const int slot = (int)a.div_B.div((uint32_t)p), e = list[slot];
+                        x.tok = e >= 0 && e < nb ? e * s.B + (p - slot * s.B) : -1;
+                    }
+                }
             }
-            const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
-            store_partial(a.part, prow, ch, D, o, inv);
+            return x;
+        };
+        struct Codes {
+            uint32_t k[KT][KWORDS], ks[KT];
+            uint4 v[VLOADS];
+            uint32_t vs[VLOADS];
+            uint32_t live;       // bit t: token t of the chunk counts
+        };
+        auto k_words = [&](const uint8_t *p, uint32_t (&w)[KWORDS]) __attribute__((always_inline)) {
+            if constexpr (KWORDS == 2) {
+                const u32x2 u = load_codes<STREAM>((const u32x2 *)p);
+                w[0] = u[0]; w[1] = u[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < KWORDS; i += 4) {
+                    const u32x4 u = load_codes<STREAM>((const u32x4 *)(p + 4 * i));
+                    w[i] = u[0]; w[i + 1] = u[1]; w[i + 2] = u[2]; w[i + 3] = u[3];
+                }
+            }
+        };
+        auto k_scale = [&](const uint8_t *p) __attribute__((always_inline)) { return SHARE == 64 ? (uint32_t) * (const uint16_t *)p : (uint32_t)*p; };
+        // Tokens that are not there are read as another of the chunk, which is; a chunk of none as token 0, and is then left out.
+        auto fetch = [&](const Tokens &tk, Codes &x) __attribute__((always_inline)) {
+            if constexpr (RUN) {
+                const int n = tk.row < 0 ? 0 : min(max(L - tk.row, 0), 32);
+                x.live = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+                const int row = n > 0 ? tk.row : 0, last = n > 0 ? n - 1 : 0;
+                const int64_t at = (int64_t)row * s.st;
+                const uint8_t *const k0 = kc + at, *const v0 = vc + at, *const ks0 = ksc + (at >> 4), *const vs0 = vsc + (at >> 4);
+                const uint32_t st = (uint32_t)s.st;   // (32 rows lie within 2^31 bytes: packed_runs)
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const uint32_t ko = (uint32_t)min(col + RT * kt, last) * st;
+                    k_words(k0 + (ko + k_lane), x.k[kt]);
+                    x.ks[kt] = k_scale(ks0 + ((ko >> 4) + ks_lane));
+                }
+#pragma unroll
+                for (int i = 0; i < VLOADS; ++i) {
+                    const uint32_t vo = (uint32_t)min(v_token(i), last) * st;
+                    x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(v0 + (vo + v_lane))));
+                    x.vs[i] = vs0[(vo >> 4) + vs_lane];
+                }
+            } else {
+                const bool there = tk.tok >= 0 && tk.tok < L;
+                const unsigned long long who = __ballot(there);
+                x.live = (uint32_t)who;
+                const int tok = there ? tk.tok : (who ? __builtin_amdgcn_readlane(tk.tok, __builtin_ctzll(who)) : 0);
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const int64_t o = (int64_t)(KT == 1 ? tok : __shfl(tok, col + RT * kt)) * s.st;
+                    k_words(kc + o + k_lane, x.k[kt]);
+                    x.ks[kt] = k_scale(ksc + (o >> 4) + ks_lane);
+                }
+#pragma unroll
+                for (int i = 0; i < VLOADS; ++i) {
+                    const int64_t vo = (int64_t)__shfl(tok, v_token(i)) * s.st;
+                    x.v[i] = __builtin_bit_cast(uint4, load_codes<STREAM>((const u32x4 *)(vc + vo + v_lane)));
+                    x.vs[i] = vsc[(vo >> 4) + vs_lane];
+                }
+            }
+        };
+
+        Acc O[OT];
+#pragma unroll
+        for (int j = 0; j < OT; ++j)
+#pragma unroll
+            for (int i = 0; i < REGS; ++i) O[j][i] = 0.f;
+        float neg_ref = 3e38f, sum_l = 0.f;   // minus the reference maximum, in log2 units; the lane's sum
+
+        // the lane's addresses for the transposing reads: its token of the four that 16 lanes turn, its 4 channels of tile j
+        uint32_t v_at[2][OT];
+        {
+            const int sl = lane & 15;
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int j = 0; j < OT; ++j) {
+                    const int t = (RT == 32 ? 8 : 16) * hf + 4 * part + (sl >> 2);
+                    const int byte = 2 * RT * j + (RT == 32 ? 32 * ((lane >> 4) & 1) : 0) + 8 * (sl & 3);   // of the row
+                    v_at[hf][j] = (uint32_t)(v_place(t, byte >> 6, (byte >> 4) & 3) + (byte & 15));
+                }
         }
-    }
-    if constexpr (SHARES) {
-        x += c1 - c0;
-        if (x >= x1) break;
-        __syncthreads();   // (the results' places are wanted again)
-    }
+        typedef __attribute__((address_space(3))) i16x4 *lds_i16x4;
+
+        auto work = [&](const Codes &x) __attribute__((always_inline)) {
+            if (x.live == 0) return;
+            // V as bf16 into LDS
+#pragma unroll
+            for (int i = 0; i < VLOADS; ++i) {
+                const int t = v_token(i);
+                const float sc = scale_of(x.vs[i]);
+                const uint32_t w[4] = {x.v[i].x, x.v[i].y, x.v[i].z, x.v[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) *(uint4 *)(mine + v_place(t, v_group, e)) = decode8_bf16(w[e], sc);
+            }
+            Acc S[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+                for (int i = 0; i < REGS; ++i) S[kt][i] = 0.f;
+#pragma unroll
+                for (int i = 0; i < STEPS; ++i) {
+                    const float sc = scale_of(SHARE == 64 ? (i >> 2 ? x.ks[kt] >> 8 : x.ks[kt] & 0xffu) : x.ks[kt]);
+                    const bf16x8 kf = __builtin_bit_cast(bf16x8, decode8_bf16(x.k[kt][i], sc));
+#pragma unroll
+                    for (int n = 0; n < N; ++n) S[kt] = Tile::mfma(kf, q[n][i], S[kt]);
+                }
+            }
+            if (x.live != 0xffffffffu) {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < REGS; ++i) S[kt][i] = x.live >> Tile::token(kt, i, part) & 1u ? S[kt][i] : -INFINITY;
+            }
+            // The reference maximum moves where the weights say that it has been left behind: one above 2^12 makes its lane's sum larger
+            // than that (so does the first chunk's, by a reference of -3e38, and one that is no number).  No maximum is looked for elsewhere.
+            float w[KT * REGS], sum;
+            auto weigh = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < KT * REGS; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(S[i / REGS][i % REGS], a.scale_log2, neg_ref));
+                // (the sum of the weights themselves, not of the rounded ones: the log-sum-exp is an output in 32 bits)
+                float t[4] = {w[0], w[1], w[2], w[3]};
+#pragma unroll
+                for (int i = 4; i < KT * REGS; ++i) t[i & 3] += w[i];
+                sum = (t[0] + t[1]) + (t[2] + t[3]);
+            };
+            weigh();
+            if (__any(!(sum <= 4096.f))) {
+                float top = S[0][0];
+#pragma unroll
+                for (int i = 1; i < KT * REGS; ++i) top = fmaxf(top, S[i / REGS][i % REGS]);
+                const float z = Tile::col_max(top) * a.scale_log2, ref = -neg_ref, ref_new = z > ref ? z : ref;
+                const float alpha = __builtin_amdgcn_exp2f(ref - ref_new);
+                neg_ref = -ref_new;
+                sum_l *= alpha;
+#pragma unroll
+                for (int j = 0; j < OT; ++j)
+#pragma unroll
+                    for (int i = 0; i < REGS; ++i) O[j][i] *= alpha;
+                weigh();
+            }
+            sum_l += sum;
+#pragma unroll
+            for (int ks = 0; ks < Tile::VSTEPS; ++ks) {
+                bf16x8 pf[N];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float f = w[8 * ks + e];
+#pragma unroll
+                    for (int n = 0; n < N; ++n) { pf[n][e] = (__bf16)f; f -= (float)pf[n][e]; }
+                }
+#pragma unroll
+                for (int j = 0; j < OT; ++j) {
+                    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[0][j] + ks * 16 * VROW));
+                    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[1][j] + ks * 16 * VROW));
+                    const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                    for (int n = 0; n < N; ++n) O[j] = Tile::mfma(vf, pf[n], O[j]);
+                }
+            }
+        };
+
+        if (c0 + wave < c1) {
+            Codes even, odd;   // (in turn, so that no registers move)
+            int c = c0 + wave;
+            fetch(tokens_of(c), even);
+            Tokens next = tokens_of(c + WAVES);
+            for (;;) {
+                fetch(next, odd);
+                next = tokens_of(c + 2 * WAVES);
+                work(even);
+                if ((c += WAVES) >= c1) break;
+                fetch(next, even);
+                next = tokens_of(c + 2 * WAVES);
+                work(odd);
+                if ((c += WAVES) >= c1) break;
+            }
+        }
+        // ---- the wavefronts' results into one: all of them to LDS, and each wavefront merges and stores every so-manieth four channels ----
+        float l = Tile::col_sum(sum_l), m = l != 0.f ? -neg_ref : -INFINITY;   // (l may be NaN)
+        ml_lds[wave][lane] = make_float2(m, l);
+        float4 *const own = (float4 *)lds[wave];     // [VALUES / 4][64]
+#pragma unroll
+        for (int i = 0; i < VALUES / 4; ++i) {
+            const Acc &o = O[4 * i / REGS];
+            own[i * 64 + lane] = make_float4(o[4 * i % REGS], o[4 * i % REGS + 1], o[4 * i % REGS + 2], o[4 * i % REGS + 3]);
+        }
+        __syncthreads();
+        float wt[WAVES];
+        m = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) m = fmaxf(m, ml_lds[x][lane].x);
+        const float ref = m == -INFINITY ? 0.f : m;
+        l = 0.f;
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) {
+            const float2 o = ml_lds[x][lane];
+            wt[x] = __builtin_amdgcn_exp2f(o.x - ref);
+            l = fmaf(o.y, wt[x], l);
+        }
+        if (row_live) {
+            const int64_t prow = slot * R + r;
+            // (the combine kernel takes a partial by l > 0: a sum that is no number is handed on in the maximum's place)
+            if (wave == 0 && part == 0) ((float2 *)a.part.ml)[prow] = l == l ? make_float2(m, l) : make_float2(l, 1.f);
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+            for (int i = 0; i < (VALUES / 4 + WAVES - 1) / WAVES; ++i) {
+                const int at = i * WAVES + wave;
+                if (at >= VALUES / 4) break;
+                float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = 0; x < WAVES; ++x) {
+                    const float4 v = ((const float4 *)lds[x])[at * 64 + lane];
+                    o[0] = fmaf(v.x, wt[x], o[0]); o[1] = fmaf(v.y, wt[x], o[1]); o[2] = fmaf(v.z, wt[x], o[2]); o[3] = fmaf(v.w, wt[x], o[3]);
+                }
+                const int ch = RT == 32 ? 32 * (at >> 2) + 8 * (at & 3) + 4 * part : 16 * at + 4 * part;   // four in a row
+                store_partial(a.part, prow, ch, D, o, inv);
+            }
+        }
+        if constexpr (SHARES) {
+            x += c1 - c0;
+            if (x >= x1) break;
+            __syncthreads();   // (the results' places are wanted again)
+        }
     } while (SHARES);
 }
 
