@@ -350,7 +350,7 @@ int specpv_pack_tokens(const specpv_kv *src, const int32_t *src_begin, const int
                        const specpv_packed_kv *dst, const int32_t *dst_begin, void *kmax, void *kmin, void *stream);
 
 /* specpv_workspace_bytes, specpv_select_blocks and specpv_partial_verify_attn for a packed cache; arguments and results are
- * theirs (all tree nodes that are keys only lie in kd / vd, in the shared dtype).  One workspace, zero-filled once, serves
+ * theirs (all tree nodes that are keys only lie in kd / vd, in the shared dtype); sel_idx and sel_count both or neither.  One workspace, zero-filled once, serves
  * packed and ordinary calls if it has the larger size.  fp32 queries and weights are taken in full (24 bits); bf16 weights are
  * rounded to bf16 in front of the product with V, as by the ordinary calls, and at head dim 128 the pieces' results travel as fp16 like theirs:
  * V entries beyond +-65504 are clamped, and results below 2^-14 are exact to 2^-25.  workspace: 16-byte aligned. */
@@ -377,7 +377,7 @@ int specpv_packed_gather_blocks(const specpv_packed_kv *kv, const int32_t *sel_i
  * times is added to m times, as the attention attends it m times).  lse [batch, Mq, Hq] is what the attention over these keys gave;
  * a row with -inf adds nothing.  Of the tree only q, M, n_q_heads and n_key_only are read; the draft's own keys have no weights.
  * weights [batch, Hkv, max_blocks * B] fp32, the caller's, zero for tokens that nothing has looked at; entries t >= L_b are left as they
- * are.  The same inputs give the same bits. */
+ * are.  nodes and n_nodes, sel_idx and sel_count: both or neither.  The same inputs give the same bits. */
 int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, const float *lse,
                               const int32_t *nodes, const int32_t *n_nodes, int32_t max_nodes,
                               const int32_t *sel_idx, const int32_t *sel_count, int32_t n_sel, float *weights, void *stream);

@@ -1005,7 +1005,7 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     const specpv_kv plain = kv_of(kv);
     if ((rc = check_tree(&plain, tree, true)) != SPECPV_OK) return rc;
     if (!out || ((uintptr_t)out & 15)) return SPECPV_EINVAL;
-    if (sel_idx && (!sel_count || n_sel < 0)) return SPECPV_EINVAL;
+    if ((sel_idx == nullptr) != (sel_count == nullptr) || (sel_idx && n_sel < 0)) return SPECPV_EINVAL;
     if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
     const PackedShape p = make_packed(kv, tree);
     const Shape &s = p.s;
@@ -1028,7 +1028,7 @@ int specpv_packed_gather_blocks(const specpv_packed_kv *kv, const int32_t *sel_i
 {
     const int rc = check_packed(kv);
     if (rc != SPECPV_OK) return rc;
-    if (!out_k || !out_v || (sel_idx && (!sel_count || n_sel < 1))) return SPECPV_EINVAL;
+    if (!out_k || !out_v || (sel_idx == nullptr) != (sel_count == nullptr) || (sel_idx && n_sel < 1)) return SPECPV_EINVAL;
     if (((uintptr_t)out_k | (uintptr_t)out_v) & 15) return SPECPV_EINVAL;
     if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
     if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;
@@ -1042,7 +1042,8 @@ int specpv_accumulate_weights(const specpv_kv *kv, const specpv_tree *tree, cons
     int rc = check_kv(kv);
     if (rc != SPECPV_OK) return rc;
     if ((rc = check_tree(kv, tree, false)) != SPECPV_OK) return rc;
-    if (!lse || !weights || (nodes && (!n_nodes || max_nodes < 1)) || (sel_idx && (!sel_count || n_sel < 0))) return SPECPV_EINVAL;
+    if (!lse || !weights || (nodes == nullptr) != (n_nodes == nullptr) || (nodes && max_nodes < 1)) return SPECPV_EINVAL;
+    if ((sel_idx == nullptr) != (sel_count == nullptr) || (sel_idx && n_sel < 0)) return SPECPV_EINVAL;
     if (nodes && max_nodes > SPECPV_MAX_M) return SPECPV_ELIMIT;
     if (sel_idx && (n_sel > (1 << 24) || (int64_t)n_sel * kv->block_size > ((int64_t)1 << 30))) return SPECPV_ELIMIT;
     if (kv->batch > 65535 || kv->n_kv_heads > 65535) return SPECPV_ELIMIT;

@@ -134,3 +134,13 @@ def test_rows_of_a_packed_allocation():
     assert lib.specpv_packed_workspace_bytes(B(p), B(_tree()), B(_cfg())) == 0
     assert lib.specpv_pack_tokens(B(_kv()), None, None, None, 4, B(p), None, None, None, None) == -1
     assert lib.specpv_packed_workspace_bytes(B(_packed(tokens=1000)), B(_tree()), B(_cfg())) == lib.specpv_packed_workspace_bytes(B(_packed()), B(_tree()), B(_cfg())) > 0
+
+
+def test_counts_without_lists():
+    """A count or a list by itself is refused (a list of no entries may come as a null pointer, and none of them means all)."""
+    lib = specpv.load()
+    assert lib.specpv_packed_verify_attn(B(_packed()), B(_tree()), None, vp(0x200), 0, vp(0x300), None, vp(0x8000), 1 << 40, None) == -1
+    assert lib.specpv_packed_gather_blocks(B(_packed()), None, vp(0x200), 0, vp(0x100), vp(0x200), None, None) == -1
+    tree = _tree(kd=None, vd=None, parent=None)
+    assert lib.specpv_accumulate_weights(B(_kv()), B(tree), vp(0x100), None, None, 0, None, vp(0x400), 0, vp(0x200), None) == -1
+    assert lib.specpv_accumulate_weights(B(_kv()), B(tree), vp(0x100), None, vp(0x400), 0, None, None, 0, vp(0x200), None) == -1

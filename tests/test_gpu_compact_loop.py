@@ -242,3 +242,24 @@ def test_offsets_beyond_32_bits(gpu_lib):
     assert all(torch.equal(a, b) for a, b in zip(*got)) and got[0][0].abs().sum() > 0 and torch.isfinite(got[0][4]).all()
     last = got[0][0][0, 0, :L - 2917 * 24].float()
     assert (last - rows[0][0, 2917 * 24:L, 0].float()).abs().max() < 1.0       # 4 bits: at most half of the last step, 2^e with e <= 0
+
+
+def test_lists_of_no_entries(gpu_lib):
+    """Tensors without an element have no address: refused, not taken for no list at all."""
+    sp = gpu_lib
+    h, _, _ = ref.cache(sp, 1, 2, 64, 128, 16, torch.bfloat16)
+    q = torch.zeros((1, 3, 4, 128), dtype=torch.bfloat16, device="cuda")
+    kd = torch.zeros((1, 3, 2, 128), dtype=torch.bfloat16, device="cuda")
+    tree = sp.Tree(q, kd, kd, torch.tensor([[-1, 0, 1]], dtype=torch.int32, device="cuda"))
+    none, cnt = torch.zeros((1, 2, 0), dtype=torch.int32, device="cuda"), torch.zeros((1, 2), dtype=torch.int32, device="cuda")
+    ws = torch.zeros((1 << 20,), dtype=torch.uint8, device="cuda")
+    empty = torch.zeros((1, 2, 0, 128), dtype=torch.bfloat16, device="cuda")
+    kv = sp.KV(*(torch.zeros((1, 2, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv"), torch.ones((1,), dtype=torch.int32, device="cuda"), 16)
+    lse, w = torch.zeros((1, 3, 4), device="cuda"), torch.zeros((1, 2, 64), device="cuda")
+    for call in (lambda: sp.specpv_packed_verify_attn(h, tree, none, cnt, torch.zeros_like(q), None, ws), lambda: sp.specpv_packed_gather_blocks(h, none, cnt, empty, empty),
+                 lambda: sp.specpv_accumulate_weights(kv, tree, lse, w, None, None, none, cnt),
+                 lambda: sp.specpv_accumulate_weights(kv, tree, lse, w, torch.zeros((1, 0), dtype=torch.int32, device="cuda"), torch.ones((1,), dtype=torch.int32, device="cuda")),
+                 lambda: sp.specpv_pack_tokens(kv, h, src_rows=torch.zeros((1, 0), dtype=torch.int32, device="cuda"))):
+        with pytest.raises(sp.SpecPVError):
+            call()
+    assert not w.any()

@@ -192,3 +192,21 @@ def test_shares_of_batches(gpu_lib, dtype, D, M, Hq, Hkv, lens, Bk):
         check(sp, h, (k, v), tree, tv, parent, ws=torch.zeros((size,), dtype=torch.uint8, device="cuda"))
     h.ctx_len.zero_()
     check(sp, h, (k, v), tree, tv, parent)
+
+
+@pytest.mark.parametrize("M", [3, 12])
+def test_rows_far_apart(gpu_lib, M):
+    """Rows 64 MiB from each other, which a chunk's 32-bit offsets do not reach: the same bits as from the same rows side by side."""
+    sp = gpu_lib
+    h, k, v = ref.cache(sp, 1, 1, 48, 128, 16, torch.bfloat16, seed=M, lens=[45])
+    far = []
+    for t, wide in ((h.k, 1 << 26), (h.v, 1 << 26), (h.k_scale, 1 << 22), (h.v_scale, 1 << 22)):
+        far.append(torch.empty((1, 1, 48, wide), dtype=torch.uint8, device="cuda")[..., :t.shape[-1]])
+        far[-1].copy_(t)
+    f = sp.PackedKV(*far, h.ctx_len, 16)
+    tree, tv, parent = _tree(sp, 1, M, 0, 4, 1, 128, torch.bfloat16, M)
+    want = check(sp, h, (k, v), tree, tv, parent)
+    got = check(sp, f, (k, v), tree, tv, parent)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    idx, cnt = _lists(1, 1, [[[2, 0, 0]]])
+    assert torch.equal(check(sp, f, (k, v), tree, tv, parent, idx, cnt)[0], check(sp, h, (k, v), tree, tv, parent, idx, cnt)[0])
