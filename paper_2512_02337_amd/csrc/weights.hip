@@ -55,8 +55,9 @@ __device__ __forceinline__ float fold32(const float (&v)[16], int lane)
     return d + __shfl_xor(d, 16);
 }
 
-// A workgroup has WAVES wavefronts, SPLIT of them to each 32 tokens, which share the tiles of query rows between them (launch_weigh).  A stage's query rows are found and fetched by all of its threads, on their way to
-// registers while the stage before is worked on; what rows cost is the less, the more wavefronts they are fetched for.
+// A workgroup has WAVES wavefronts, SPLIT of them to each 32 tokens, which share the tiles of query rows between them (launch_weigh).  A
+// stage's query rows are found and fetched by all of its threads, on their way to registers while the stage before is worked on; what rows
+// cost is the less, the more wavefronts they are fetched for.
 template <typename T, int D, int WAVES, int SPLIT> struct WeighTile {
     static constexpr int E = Elem<T>::kPerVec, STEPS = D / (2 * E);        // channels of a lane's 16 bytes; products of a tile
     static constexpr int PIECES = D / E;                                   // 16-byte pieces of a row
