@@ -18,7 +18,7 @@ struct WeighKernelArgs {
     Shape s;
     WeighArgs a;
     FastDiv div_B, div_G;
-    float scale_log2;
+    float scale_log2, scale_off;   // log2 e / sqrt(D), and by what part of itself it is too small
 };
 
 template <typename T> struct Mfma32;
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
     typedef WeighTile<T, D, WAVES, SPLIT> W;
     constexpr int STEPS = W::STEPS, THREADS = 64 * WAVES;
     __shared__ uint4 q_lds[2][W::ROWS * W::PIECES];
-    __shared__ float lse_lds[2][W::ROWS];   // -lse * log2 e; -inf: no such row
+    __shared__ float2 lse_lds[2][W::ROWS];   // -lse * log2 e; -inf: no such row.  And what that is off by, as a factor (below)
     const Shape &s = k.s;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int g = blockIdx.y, b = blockIdx.z, half = lane >> 5, col = lane & 31;
@@ -111,24 +111,29 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
     // ---- query rows r0 .. r0 + ROWS - 1: this thread's pieces, and the sums of the rows whose first pieces they are ----
     const int nodes = k.a.nodes ? min(k.a.n_nodes[b], k.a.max_nodes) : s.M;
     const int R = max(nodes, 0) * s.G;
+    // A weight is 2^x, x = z - lse * log2 e, and large where the two nearly cancel: what either is off by from its rounding is then larger than x's own
+    // error.  The product with lse comes in two parts, and z = scale_log2 * (1 + scale_off) * q . k is -lse * log2 e's opposite but for x: both
+    // offsets are a factor of the row, which the sums take in without another instruction.
     uint4 qp[W::MINE];
-    float neg[W::MINE];
+    float2 neg[W::MINE];
+    auto row_of = [&](float l) {
+        const float n = l * -kLog2e, low = fmaf(l, -kLog2e, -n) - l * 1.925963033500011e-8f;   // (log2 e itself less kLog2e)
+        if (l == -INFINITY) return make_float2(-INFINITY, 1.f);                                  // (a row that attended nothing gives nothing)
+        return make_float2(n, fabsf(n) < 1e6f ? fmaf(0.693147181f, low - k.scale_off * n, 1.f) : 1.f);   // (beyond, nothing cancels)
+    };
     auto fetch = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < W::MINE; ++x) {
             const int at = (int)threadIdx.x + x * THREADS, row = r0 + at / W::PIECES, piece = at % W::PIECES;
             qp[x] = make_uint4(0, 0, 0, 0);
-            neg[x] = -INFINITY;
+            neg[x] = make_float2(-INFINITY, 1.f);
             if (row < R) {
                 const int i = (int)k.div_G.div((uint32_t)row), hh = row - i * s.G;
                 const int node = k.a.nodes ? k.a.nodes[(int64_t)b * k.a.max_nodes + i] : i;
                 if (node >= 0 && node < s.M) {
                     const int64_t qr = ((int64_t)b * s.M + node) * s.Hq + (int64_t)g * s.G + hh;
                     qp[x] = ((const uint4 *)s.q)[qr * W::PIECES + piece];
-                    if (piece == 0) {
-                        const float l = k.a.lse[qr];
-                        neg[x] = l == -INFINITY ? -INFINITY : l * -kLog2e;   // (a row that attended nothing gives nothing)
-                    }
+                    if (piece == 0) neg[x] = row_of(k.a.lse[qr]);
                 }
             }
         }
@@ -156,9 +161,9 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
             for (int i = 0; i < 16; ++i) sc[i] = 0.f;
 #pragma unroll
             for (int i = 0; i < STEPS; ++i) sc = Mfma32<T>::step(kk[i], q_lds[buf][W::place(t0 + col, 2 * i + half)], sc);
-            const float n = lse_lds[buf][t0 + col];
+            const float2 n = lse_lds[buf][t0 + col];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(sc[i], k.scale_log2, n));
+            for (int i = 0; i < 16; ++i) sum[i] = fmaf(__builtin_amdgcn_exp2f(fmaf(sc[i], k.scale_log2, n.x)), n.y, sum[i]);
         }
     }
     // ---- fold the columns; value i of a tile is its token 8 * (i >> 2) + 4 * half + (i & 3) ----
@@ -182,7 +187,8 @@ __global__ __launch_bounds__(64 * WAVES) void weigh_kernel(WeighKernelArgs k)
 
 hipError_t launch_weigh(const Shape &s, int dtype, const WeighArgs &a, hipStream_t st)
 {
-    const WeighKernelArgs k{s, a, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.G), kLog2e / sqrtf((float)s.D)};
+    const double scale = 1.4426950408889634 / sqrt((double)s.D);
+    const WeighKernelArgs k{s, a, make_fastdiv((uint32_t)s.B), make_fastdiv((uint32_t)s.G), (float)scale, (float)(scale / (float)scale - 1.)};
     const int64_t positions = (a.sel_idx ? (int64_t)a.n_sel : (int64_t)s.max_blocks) * s.B;
     if (positions <= 0) return hipSuccess;
     const int64_t rows = (int64_t)(a.nodes ? a.max_nodes : s.M) * s.G;
