@@ -263,3 +263,49 @@ def test_lists_of_no_entries(gpu_lib):
         with pytest.raises(sp.SpecPVError):
             call()
     assert not w.any()
+
+
+def test_replays_follow_the_lengths(gpu_lib):
+    """A batch whose sequences grow and shrink between the replays of one graph: each replay gives what an eager call gives."""
+    sp = gpu_lib
+    g = torch.Generator(device="cuda").manual_seed(9)
+    T, Hk, Dh = 13056, 2, 64
+    rows = [torch.randn((3, Hk, T, Dh), generator=g, device="cuda").bfloat16() for _ in "kv"]
+    lens = torch.tensor([13000, 700, 1], dtype=torch.int32, device="cuda")
+    z = lambda w: torch.zeros((3, Hk, T, w), dtype=torch.uint8, device="cuda")  # noqa: E731
+    p = sp.PackedKV(z(32), z(32), z(2), z(2), torch.full((3,), T, dtype=torch.int32, device="cuda"), 64)
+    full = sp.KV(rows[0], rows[1], torch.full((3,), T, dtype=torch.int32, device="cuda"), 64)
+    sp.specpv_pack_tokens(full, p)
+    p.ctx_len.copy_(lens)
+    kv = sp.KV(rows[0], rows[1], p.ctx_len, 64)
+    q = torch.randn((3, 60, 10, Dh), generator=g, device="cuda").bfloat16()
+    kd, vd = (torch.randn((3, 60, Hk, Dh), generator=g, device="cuda").bfloat16() for _ in "kv")
+    tree = sp.Tree(q, kd, vd, torch.arange(-1, 59, dtype=torch.int32, device="cuda").expand(3, -1).contiguous())
+    ws = torch.zeros((max(sp.specpv_packed_workspace_bytes(p, tree), sp.specpv_evict_workspace_bytes(kv)),), dtype=torch.uint8, device="cuda")
+    dst = sp.KV(*(torch.zeros((3, Hk, 704, Dh), dtype=torch.bfloat16, device="cuda") for _ in "kv"), torch.zeros((3,), dtype=torch.int32, device="cuda"), 64)
+    o = dict(out=torch.zeros_like(q), lse=torch.zeros((3, 60, 10), device="cuda"), w=torch.zeros((3, Hk, T), device="cuda"),
+             idx=torch.zeros((3, Hk, 700), dtype=torch.int32, device="cuda"), k=dst.k, v=dst.v, n=dst.ctx_len)
+
+    def run():
+        o["w"].zero_()
+        sp.specpv_packed_verify_attn(p, tree, None, None, o["out"], o["lse"], ws)
+        sp.specpv_accumulate_weights(kv, tree, o["lse"], o["w"])
+        sp.specpv_evict_tokens(kv, o["w"], 4, 96, 600, dst, o["idx"], None, ws)
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for now in ([13000, 700, 1], [5, 13056, 6000], [0, 0, 0], [13056, 13056, 13056], [699, 701, 700]):
+        p.ctx_len.copy_(torch.tensor(now, dtype=torch.int32))
+        for t in o.values():
+            t.zero_()
+        run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in o.values()]
+        for t in o.values():
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o.values(), want)), now
+        assert o["n"].tolist() == [min(L, 700) for L in now]

@@ -210,3 +210,13 @@ def test_rows_far_apart(gpu_lib, M):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     idx, cnt = _lists(1, 1, [[[2, 0, 0]]])
     assert torch.equal(check(sp, f, (k, v), tree, tv, parent, idx, cnt)[0], check(sp, h, (k, v), tree, tv, parent, idx, cnt)[0])
+
+
+@pytest.mark.parametrize("dtype,D,M,n_key,Hq,Hkv,lens", [(torch.bfloat16, 128, 60, 5, 10, 2, [1, 12000, 4000, 8999]), (torch.float32, 64, 60, 17, 10, 2, [13000, 0, 33]),
+                                                         (torch.bfloat16, 64, 20, 3, 8, 2, [700, 90]), (torch.bfloat16, 128, 3, 18, 8, 2, [3000])])
+def test_key_only_nodes_over_whole_caches(gpu_lib, dtype, D, M, n_key, Hq, Hkv, lens):
+    sp = gpu_lib
+    T = -(-max(lens) // 64) * 64
+    h, k, v = ref.cache(sp, len(lens), Hkv, T, D, 64, dtype, seed=M, lens=lens)
+    tree, tv, parent = _tree(sp, len(lens), M, n_key, Hq, Hkv, D, dtype, M + D)
+    check(sp, h, (k, v), tree, tv, parent)
