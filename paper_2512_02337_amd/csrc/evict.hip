@@ -357,8 +357,9 @@ __global__ __launch_bounds__(64 * kWaves) void resolve_kernel(EvictKernelArgs k)
     uint32_t key[kKeys];
     load_keys<kKeys, kWaves>(s, t0, key);
     if (g == 0 && blockIdx.x == 0 && tid == 0) const_cast<int32_t *>(k.d.ctx_len)[b] = min(s.L, s.n_keep);
-    if (s.all()) {
-        for (int i = t0 + tid; i < min(s.n_keep, t0 + kChunk); i += 64 * kWaves) s.idx[i] = i < s.L ? i : -1;
+    if (s.all()) {   // (the grid has the source's chunks, and more tokens may stay than it has room for)
+        for (int64_t c = t0; c < s.n_keep; c += (int64_t)gridDim.x * kChunk)
+            for (int i = (int)c + tid; i < min(s.n_keep, (int)c + kChunk); i += 64 * kWaves) s.idx[i] = i < s.L ? i : -1;
         return;
     }
     if (t0 >= s.L) return;
