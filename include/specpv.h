@@ -331,7 +331,8 @@ typedef struct specpv_packed_kv {
     int32_t max_blocks;
     specpv_dtype dtype;
     int32_t tokens;         /* rows that the allocation has, where those are fewer than max_blocks * block_size; 0: that many.
-                               None behind them is written                                */
+                               None behind them is read or written; a ctx_len beyond them counts
+                               as that many                                               */
 } specpv_packed_kv;
 
 /* Rows of src (an ordinary cache, a chunk of a prompt, the draft's buffer) into a packed cache.  For sequence b and

@@ -13,7 +13,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 struct PackedShape {
     Shape s;                     // k, v: codes; sb, sh, st: bytes of codes (a sixteenth of them for the scales)
     const uint8_t *ks, *vs;
-    int64_t rows;                // that may be written
+    int64_t rows;                // that the memory has: none behind them is read or written, whatever the lengths say
 };
 
 constexpr int kPackedGroup = 32;       // channels of a scale

@@ -103,7 +103,6 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
     const Shape &s = a.p.s;
     const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & (RT - 1), part = lane / RT;
-    const int64_t cap = (int64_t)s.max_blocks * s.B;
     const int R = s.M * s.G;
     int x = 0, x1 = 0, seq_chunks = 0, seq_upto = 0;   // SHARES: chunks from here to there, in the row of all pairs' (and see StreamShare)
     if constexpr (SHARES) {
@@ -134,7 +133,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
         }
         const int r = tile * RT + col;
         const bool row_live = r < R;
-        const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
+        const int L = (int)min((int64_t)max(s.ctx_len[b], 0), a.p.rows);   // (SHARES: chunks behind it have nothing)
         const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
         int span = L;
         if (a.sel_idx) span = L ? max(min(a.sel_count[bg], a.n_sel), 0) * s.B : 0;

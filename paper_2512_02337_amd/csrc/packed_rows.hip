@@ -193,8 +193,7 @@ __global__ __launch_bounds__(256) void packed_gather_kernel(PackedGatherArgs a)
     constexpr int LPR = D / 8, RPP = 256 / LPR, U = 4;
     const Shape &s = a.p.s;
     const int g = blockIdx.y, b = blockIdx.z;
-    const int64_t cap = (int64_t)s.max_blocks * s.B;
-    const int L = (int)min((int64_t)max(s.ctx_len[b], 0), cap);
+    const int L = (int)min((int64_t)max(s.ctx_len[b], 0), a.p.rows);
     const int nb = (int)a.div_B.div((uint32_t)L + (uint32_t)s.B - 1u);
     if (blockIdx.x == 0) {
         if (g || !a.out_len) return;
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(256) void packed_gather_kernel(PackedGatherArgs a)
         if (threadIdx.x == 0) a.out_len[b] = max(max(most[0], most[1]), max(most[2], most[3]));
         return;
     }
-    const int64_t bg = (int64_t)b * s.Hkv + g, total = a.sel_idx ? (int64_t)a.n_sel * s.B : cap;
+    const int64_t bg = (int64_t)b * s.Hkv + g, total = (a.sel_idx ? (int64_t)a.n_sel : (int64_t)s.max_blocks) * s.B;
     const int cnt = a.sel_idx ? a.sel_count[bg] : 0;
     const int c = threadIdx.x % LPR, rsub = threadIdx.x / LPR;
     const int64_t src0 = (int64_t)b * s.sb + (int64_t)g * s.sh;
