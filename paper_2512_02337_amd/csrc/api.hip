@@ -693,7 +693,8 @@ static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks, bool 
     if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;
     if (ns > 64) ns = 64;
     const int64_t stream = cus / packed_row_tiles(s, dtype), behind = (int64_t)s.batch * (s.batch + 1) / 2 * s.Hkv;
-    if (!lists && s.batch >= 3 && s.batch <= 64 && stream > 0 && packed_runs(s, false) && chunks * s.batch * s.Hkv >= 64 * (stream + behind)) return {1, stream, 8};
+    const int64_t all = chunks * s.batch * s.Hkv;   // (StreamShare counts them in 32 bits)
+    if (!lists && s.batch >= 3 && s.batch <= 64 && stream > 0 && packed_runs(s, false) && all >= 64 * (stream + behind) && all < ((int64_t)1 << 30)) return {1, stream, 8};
     return {ns < 1 ? 1 : ns, 0, waves};
 }
 
