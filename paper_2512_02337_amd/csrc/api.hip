@@ -1012,6 +1012,7 @@ int specpv_packed_verify_attn(const specpv_packed_kv *kv, const specpv_tree *tre
     const Shape &s = p.s;
     if ((uintptr_t)workspace & 15) return SPECPV_EINVAL;
     const int64_t pairs = (int64_t)s.batch * s.Hkv;
+    if (pairs > 8 * (int64_t)65535) return SPECPV_ELIMIT;   // the combine kernel's grid, before anything is enqueued
     if (!workspace || workspace_bytes < packed_bytes(s, kv->dtype, pairs)) return SPECPV_EWORKSPACE;
     PackedPlan plan = packed_plan(s, kv->dtype, sel_idx ? n_sel : s.max_blocks, sel_idx != nullptr);
     while (plan.partials(s) > pairs && packed_bytes(s, kv->dtype, plan.partials(s)) > workspace_bytes) --(plan.stream ? plan.stream : plan.ns);

@@ -31,3 +31,11 @@ def test_chunks_of_all_sequences_are_counted_in_32_bits():
     assert _slots(3, 10, 1 << 20) == 256 + 30                  # 30 * 2^25 chunks: less than 2^30
     for batch, Hkv, splits in ((4, 8, 8), (16, 16, 1), (64, 2, 2), (64, 64, 1)):
         assert _slots(batch, Hkv, 1 << 20) == splits * batch * Hkv, (batch, Hkv)
+
+
+def test_more_pairs_than_the_second_launch_has_room_for():
+    """Refused before the first one is enqueued."""
+    def call(batch, Hkv):
+        p = _packed(batch=batch, n_kv_heads=Hkv, stride_h=0, stride_b=0)
+        return specpv.load().specpv_packed_verify_attn(B(p), B(_tree(M=1, n_q_heads=Hkv)), None, None, 0, vp(0x300), None, vp(0x8000), 1 << 60, None)
+    assert call(65536, 8) == -3 and call(1, 524281) == -3
