@@ -352,8 +352,8 @@ int specpv_pack_tokens(const specpv_kv *src, const int32_t *src_begin, const int
 
 /* specpv_workspace_bytes, specpv_select_blocks and specpv_partial_verify_attn for a packed cache; arguments and results are
  * theirs (all tree nodes that are keys only lie in kd / vd, in the shared dtype); sel_idx and sel_count both or neither.  One workspace, zero-filled once, serves
- * packed and ordinary calls if it has the larger size.  fp32 queries and weights are taken in full (24 bits); bf16 weights are
- * rounded to bf16 in front of the product with V, as by the ordinary calls, and at head dim 128 the pieces' results travel as fp16 like theirs:
+ * packed and ordinary calls if it has the larger size.  fp32 queries and weights are taken in full (24 bits), bf16 weights
+ * at head dim 64 too; at 128 they are rounded to bf16 in front of the product with V, and the pieces' results travel as fp16, both as in the ordinary calls:
  * V entries beyond +-65504 are clamped, and results below 2^-14 are exact to 2^-25.  workspace: 16-byte aligned. */
 size_t specpv_packed_workspace_bytes(const specpv_packed_kv *kv, const specpv_tree *tree, const specpv_select_cfg *cfg);
 int specpv_packed_select_blocks(const specpv_packed_kv *kv, const specpv_tree *tree, const void *kmax, const void *kmin,

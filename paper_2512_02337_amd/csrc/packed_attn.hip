@@ -27,8 +27,11 @@ struct PackedAttnArgs {
 };
 
 
-// One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.
-template <typename T> struct Pieces { static constexpr int N = sizeof(T) == 2 ? 1 : 3; };
+// One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.  Queries are as they come.  The weights have
+// what they have in the ordinary calls: all 24 bits for fp32 and for bf16 at 64 channels (one operand / three: 60 query tokens x 4 heads over 32K,
+// 8 KV heads, 30.4 / 44.0 us, one over 128K 18.3 / 20.0), bf16's 8 at 128 (one / two: 78 over 64K 109.8 / 142.2, 60 over a list of 4K 16.3 /
+// 17.6, one over 128K 29.2 / 30.0; outputs off by 0.0023 / 0.0017 of their size, where their own rounding is 0.0017).
+template <typename T, int D> struct Pieces { static constexpr int Q = sizeof(T) == 2 ? 1 : 3, W = sizeof(T) == 2 && D == 128 ? 1 : 3; };
 
 // Which tokens a chunk has.  RUN: they follow each other in memory (the whole cache, or blocks of whole chunks): a scalar row and a
 // count.  Else (blocks of other sizes) a lane looks its token up.
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
 {
     typedef RowTile<RT, D> Tile;
     typedef typename Tile::Acc Acc;
-    constexpr int N = Pieces<T>::N, GROUPS = D / 32, KT = Tile::KT, REGS = Tile::REGS;
+    constexpr int N = Pieces<T, D>::Q, NW = Pieces<T, D>::W, GROUPS = D / 32, KT = Tile::KT, REGS = Tile::REGS;
     constexpr int PARTS = 64 / RT, SHARE = D / PARTS, STEPS = SHARE / 8;   // lanes of a column; their channels, and steps of the product
     constexpr int KWORDS = SHARE / 8;                 // 4-byte words of K codes of a lane and tile
     constexpr int OT = D / RT, VLOADS = D / 64;
@@ -346,22 +349,29 @@ __global__ __launch_bounds__(64 * WAVES, 2) void packed_attn_kernel(PackedAttnAr
                 weigh();
             }
             sum_l += sum;
+            const Bf16Halves halves;
 #pragma unroll
             for (int ks = 0; ks < Tile::VSTEPS; ++ks) {
-                bf16x8 pf[N];
+                uint32_t pk[NW][4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float f = w[8 * ks + e];
+                for (int e = 0; e < 4; ++e) {
+                    float f0 = w[8 * ks + 2 * e], f1 = w[8 * ks + 2 * e + 1];
 #pragma unroll
-                    for (int n = 0; n < N; ++n) { pf[n][e] = (__bf16)f; f -= (float)pf[n][e]; }
+                    for (int n = 0; n < NW; ++n) {
+                        pk[n][e] = pack_bf16x2(f0, f1);
+                        if (n + 1 < NW) { f0 = halves.sub_lo(f0, pk[n][e]); f1 = halves.sub_hi(f1, pk[n][e]); }
+                    }
                 }
+                bf16x8 pf[NW];
+#pragma unroll
+                for (int n = 0; n < NW; ++n) pf[n] = __builtin_bit_cast(bf16x8, make_uint4(pk[n][0], pk[n][1], pk[n][2], pk[n][3]));
 #pragma unroll
                 for (int j = 0; j < OT; ++j) {
                     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[0][j] + ks * 16 * VROW));
                     const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(mine + v_at[1][j] + ks * 16 * VROW));
                     const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-                    for (int n = 0; n < N; ++n) O[j] = Tile::mfma(vf, pf[n], O[j]);
+                    for (int n = 0; n < NW; ++n) O[j] = Tile::mfma(vf, pf[n], O[j]);
                 }
             }
         };
