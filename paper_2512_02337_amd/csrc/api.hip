@@ -669,9 +669,12 @@ static size_t packed_bytes(const Shape &s, int dtype, int64_t partials)   // (of
 // rows; else four, whose results are merged sooner.  (us, 8 KV heads, 4 / 8: 60 query tokens x 4 heads 2K 11.4 / 12.0, 4K 13.7 / 13.5, 16K 33.7 / 27.6, 64K
 // 108.5 / 83.3; 30, 4K 10.9 / 11.3, 16K 21.3 / 18.9; 8, 16K 12.4 / 12.6, 64K 23.0 / 20.4; fp32, 128 channels, 4, 2K 8.1 / 8.8, 16K 12.9 / 13.5, 64K 25.8 / 22.8; 16,
 // 2K 9.6 / 10.3, 16K 23.7 / 21.5; bf16, one token, 2K 7.8 / 7.5, 8K 10.0 / 9.9, 32K 14.6 / 14.1, 128K 32.0 / 30.7, and 12: 8.0, 10.6, 14.9, 30.9.)
+// Four too where there are more columns than CUs, however long they are: two workgroups share a CU then (60 query tokens x 4 heads, 8 KV heads, 8 sequences,
+// lists of 512, 1K, 4K, 8K tokens, 4 / 8: 18.1 / 22.2, 22.9 / 26.5, 49.9 / 53.7, 86.4 / 90.4; 64 channels, 16 of 2K 48.2 / 56.5; fp32, 16 of 4K, two KV heads 77 / 91).
 // Where one workgroup to a CU leaves a third of the CUs idle, twice as many, of four wavefronts where there are such (20 sequences of 8K, one token: 38.4 /
 // 34.6; of 4K, 8 tokens: 33.2 / 25.0; 12 of 8K, a quarter idle: 23.2 / 26.2).  No more than a split to four chunks, and 64 (two KV heads, 64K, 32 / 64 / 128:
-// 17.1 / 15.1 / 17.1).
+// 17.1 / 15.1 / 17.1).  Few columns, whose 64 splits leave a third idle for good, keep the four (8 tokens x 4 heads, one KV head, 4 / 8: 32K 13.0 / 13.5, 64K 16.2 /
+// 15.8, 128K 21.9 / 20.2; fp32, 2 tokens, 16K 11.4 / 11.9, 64K 17.5 / 16.6).
 // Whole caches of three sequences and more: one share of all chunks to a CU instead (StreamShare), however long each sequence is, where a share is long against
 // what each pair in it costs, taking the batch for one of lengths 1 : 2 : 3 : ..., whose shortest come several to a share.  (us, splits / shares,
 // lengths 1 : 2 : ... and equal, 8 KV heads: 60 query tokens, 8 x 32K 281 / 209 and 321 / 322; 73, 3 x 35K 155 / 130 and 165 / 181; one, 8 x 32K 40.6 / 33.4
@@ -687,7 +690,7 @@ static PackedPlan packed_plan(const Shape &s, int dtype, int64_t n_blocks, bool 
     const int64_t tokens = (n_blocks < s.max_blocks ? n_blocks : (int64_t)s.max_blocks) * s.B, chunks = (tokens + 31) / 32;
     const int64_t columns = (int64_t)s.batch * s.Hkv * packed_row_tiles(s, dtype), cus = device_cu_count();
     int64_t ns = cus / columns;
-    const bool idle = 3 * ns * columns < 2 * cus, few = dtype == SPECPV_BF16 && packed_row_tile(s, dtype) == 16;
+    const bool idle = 3 * ns * columns < 2 * cus /* (more columns than CUs: ns = 0) */, few = dtype == SPECPV_BF16 && packed_row_tile(s, dtype) == 16;
     const int waves = few || (!idle && chunks >= 32 * ns) ? 8 : 4;
     if (idle) ns = 2 * cus / columns;
     if (ns > (chunks + 3) / 4) ns = (chunks + 3) / 4;

@@ -8,7 +8,7 @@
 // piece of LDS of its own as bf16, because its operand has tokens where memory has channels: the transposing LDS reads turn it.
 // Bound by memory for few rows (one token over 8 heads of 128K, 142 MB: 25.2 us, 5.6 TB/s), by matrix and vector units at the clock that the
 // chip's power leaves for many (78 over 64K: 105 us, 800 TFLOP/s at 1.55 GHz).
-// The next chunk's codes, 35 bytes a lane, are under way while one is worked on.  (Two of them: 13.8 us for 12.9 over 32K tokens, 30.5 for
+// The next chunk's codes, 68 bytes a lane at 128 channels, are under way while one is worked on.  (Two of them: 13.8 us for 12.9 over 32K tokens, 30.5 for
 // 29.1 over 128K, 50.6 for 49.0 over 32 sequences of 8K: a split's end reads more for nothing, and there are wavefronts enough.)
 #include "packed.h"
 #include "attn_mfma.h"
