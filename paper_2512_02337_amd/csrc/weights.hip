@@ -5,7 +5,7 @@
 // a wavefront keeps its tokens' K rows in registers as the matrix instruction's A operand (rows = tokens), the query rows go
 // by as B (columns), 32 at a time out of LDS, and a lane adds up its column's weights for 16 tokens a tile.  The 32 columns
 // are folded once, at the end.  K is read once and nothing else of size is read or written: few rows are bound by that (16 rows over
-// 8 heads of 128K, bf16, 268 MB: 52.5 us, 5.1 TB/s), many by products, exponentials and LDS reads together (512 rows over 32K: 46 - 50 us, 690 -
+// 8 heads of 128K, bf16, 268 MB: 53.3 us, 5.0 TB/s), many by products, exponentials and LDS reads together (512 rows over 32K: 46 - 50 us, 690 -
 // 740 TFLOP/s; without the exponentials a workgroup takes 77 % of its cycles, without the products 86, without the LDS reads 82).
 #include "summarize.h"
 
