@@ -27,7 +27,7 @@ struct PackedAttnArgs {
 };
 
 
-// One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.  Queries are as they come.  The weights have
+// One or three bf16 operands whose sum is the value: fp32 has 24 significant bits, bf16 8.  Queries have all of theirs, the weights
 // what they have in the ordinary calls: all 24 bits for fp32 and for bf16 at 64 channels (one operand / three: 60 query tokens x 4 heads over 32K,
 // 8 KV heads, 30.4 / 44.0 us, one over 128K 18.3 / 20.0), bf16's 8 at 128 (one / two: 78 over 64K 109.8 / 142.2, 60 over a list of 4K 16.3 /
 // 17.6, one over 128K 29.2 / 30.0; outputs off by 0.0023 / 0.0017 of their size, where their own rounding is 0.0017).
